@@ -55,7 +55,9 @@ typedef enum {
     BCQ_ERR_BAD_SHAPE = -3,  /* m, n, batch or group violate the shape rules */
     BCQ_ERR_ALIGN = -4,      /* a pointer is not aligned as required */
     BCQ_ERR_HIP = -5,        /* the HIP runtime reported an error at launch */
-    BCQ_ERR_VARIANT = -6     /* a forced kernel variant cannot run this problem */
+    BCQ_ERR_VARIANT = -6,    /* a forced kernel variant cannot run this problem */
+    BCQ_ERR_BAD_TYPE = -7,   /* a bcq_type or bcq_activation out of range */
+    BCQ_ERR_WORKSPACE = -8   /* the workspace is smaller than the call needs */
 } bcq_status;
 
 /* Static, NUL-terminated description of a status code.  Host call. */
@@ -210,6 +212,77 @@ enum { BCQ_RESIDUAL_FROZEN_PLANES = 0, BCQ_RESIDUAL_LISTING = 1 };
 int bcq_quantize_form(const bcq_half *w, int p_low, int p_high, int cycles, int residual_form, uint32_t *planes,
                       bcq_half *const *scales_by_p, bcq_half *const *offsets_by_p, int64_t m, int64_t n, int group,
                       void *stream);
+
+/*
+ * 8-bit operators.  Beside the bit-plane products, for layers that stand no fewer bits and for prompts, whose products are bound by
+ * arithmetic: weights and activations as int8 codes with one fp32 scale per output channel and one per token.
+ *   q        int8 [tokens][n], token_scales float [tokens]: token t's activations are token_scales[t] * q[t][j]
+ *   w        int8 [m][n], channel_scales float [m]: output channel r's weights are channel_scales[r] * w[r][j]
+ * bcq_int8_quantize makes both from 16-bit rows.  Any int8 value is a legal code.  16-bit tensors are binary16 or bfloat16 (`type`).
+ *
+ * Shape rules: 1 <= m <= 2^24 (backward passes: 2^20), 16 <= n <= 131056, n % 16 == 0 (a sum of n products of two codes fits 32 bits), 0 <= tokens <= 2^24,
+ * m * tokens <= 2^40.  q, w, x and dx must be 16-byte aligned, y, h, dy and dh 2-byte, scales 4-byte.  No tokens: the forward calls do nothing (their per-token pointers
+ * may be NULL), the backward calls write zeros to the scales' gradients.
+ * Sums over columns are exact (32-bit integers), everything behind them is fp32, and results are rounded once to 16 bits.  Results do not depend
+ * on what else is in the call's batch.
+ */
+typedef enum { BCQ_FLOAT16 = 0, BCQ_BFLOAT16 = 1 } bcq_type;
+typedef enum {
+    BCQ_ACT_SILU = 0,       /* g / (1 + exp(-g)) */
+    BCQ_ACT_GELU = 1        /* g / (1 + exp(-2 z)), z = sqrt(2 / pi) (g + 0.044715 g^3): the tanh form of gelu */
+} bcq_activation;
+
+/*
+ * bcq_int8_quantize -- rows to 8 bits:  scales[t] = max_j |x[t][j]| / 127,  q[t][j] = 127 x[t][j] / max |x[t]| rounded to the nearest
+ * whole number, ties to even, as in exact arithmetic.  A row of zeros gets scale 0 and codes 0; a row that holds a NaN or an infinity gets scale NaN and
+ * codes 0, so that what is computed from it is NaN and no other row is touched.
+ *   x       [rows][n] of `type`
+ *   q       int8 [rows][n] (written), scales float [rows] (written)
+ * Activations: a row per token, at run time.  Weights: a row per output channel, offline.
+ */
+int bcq_int8_quantize(const void *x, int type, int8_t *q, float *scales, int64_t rows, int64_t n, void *stream);
+
+/*
+ * bcq_int8_gemm -- y[t][r] = token_scales[t] * channel_scales[r] * sum_j q[t][j] w[r][j]
+ *   y       [tokens][m] of `type` (written)
+ */
+int bcq_int8_gemm(const int8_t *q, const float *token_scales, const int8_t *w, const float *channel_scales, void *y, int type,
+                  int64_t m, int64_t n, int64_t tokens, void *stream);
+
+/*
+ * bcq_int8_gated -- the gated feed-forward block up to its down projection, both projections, the activation and the product in one kernel:
+ *     h[t][r] = act(g[t][r]) * u[t][r],   g = bcq_int8_gemm with w_gate, u with w_up (neither is rounded)
+ *   h       [tokens][m] of `type` (written)
+ */
+int bcq_int8_gated(const int8_t *q, const float *token_scales, const int8_t *w_gate, const float *gate_scales, const int8_t *w_up,
+                   const float *up_scales, int activation, void *h, int type, int64_t m, int64_t n, int64_t tokens, void *stream);
+
+/*
+ * Backward passes, the codes fixed: gradients of the activations (through the quantiser as if it were the identity) and of the channel
+ * scales, which are what tuning with fixed codes trains.
+ *
+ * bcq_int8_gemm_backward:
+ *     dx[t][j] = sum_r dy[t][r] channel_scales[r] w[r][j]
+ *     dchannel_scales[r] = sum_t dy[t][r] token_scales[t] sum_j q[t][j] w[r][j]
+ * bcq_int8_gated_backward: with dg = dh u act'(g) and du = dh act(g) (g and u are computed again)
+ *     dx[t][j] = sum_r dg[t][r] gate_scales[r] w_gate[r][j] + du[t][r] up_scales[r] w_up[r][j]
+ *     dgate_scales[r] = sum_t dg[t][r] token_scales[t] sum_j q[t][j] w_gate[r][j],   dup_scales likewise with du and w_up
+ *   dy, dh      [tokens][m] of `type`
+ *   dx          [tokens][n] of `type` (written); gradients of the scales: float [m] (written)
+ *   workspace   at least bcq_int8_backward_workspace(matrices, m, tokens) bytes, 256-byte aligned, contents irrelevant before
+ *               and after; matrices: 1 for bcq_int8_gemm_backward, 2 for bcq_int8_gated_backward.  Calls that may run at the same time
+ *               need one each.
+ * The gradients of the projections are held in 11 bits on their way into the product with the weights, scaled per token so that dy's range does
+ * not matter.  Sums have a fixed order: the same call gives the same bits.
+ * bcq_int8_backward_workspace returns BCQ_ERR_BAD_SHAPE for sizes that the calls refuse.  Host call.
+ */
+int64_t bcq_int8_backward_workspace(int matrices, int64_t m, int64_t tokens);
+int bcq_int8_gemm_backward(const void *dy, const int8_t *q, const float *token_scales, const int8_t *w, const float *channel_scales,
+                           void *dx, float *dchannel_scales, int type, int64_t m, int64_t n, int64_t tokens, void *workspace,
+                           int64_t workspace_bytes, void *stream);
+int bcq_int8_gated_backward(const void *dh, const int8_t *q, const float *token_scales, const int8_t *w_gate, const float *gate_scales,
+                            const int8_t *w_up, const float *up_scales, int activation, void *dx, float *dgate_scales, float *dup_scales,
+                            int type, int64_t m, int64_t n, int64_t tokens, void *workspace, int64_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

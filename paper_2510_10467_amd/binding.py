@@ -23,6 +23,8 @@ _host = None
 
 BCQ_MAX_PLANES = 8
 KERNEL_AUTO, KERNEL_SIGN_SELECT, KERNEL_PLANE_MFMA, KERNEL_DEQUANT_MFMA = 0, 1, 2, 3
+TYPES = {torch.float16: 0, torch.bfloat16: 1}           # bcq_type
+ACTIVATIONS = {"silu": 0, "gelu": 1}                    # bcq_activation
 KERNEL_IDS = {"auto": 0, "sign_select": 1, "plane_mfma": 2, "dequant_mfma": 3, "plane_f16": 4, "lut": 5}
 
 
@@ -34,10 +36,10 @@ class BcqError(RuntimeError):
 
 class _NoHost:
     """In the place of ``_bcq_host``: declines every call, so that the Python code makes it."""
-    gemv = gemv_multi = gemm_mixed = staticmethod(lambda *args: None)
+    gemv = gemv_multi = gemm_mixed = int8_quantize = int8_gemm = int8_gated = staticmethod(lambda *args: None)
 
 
-def _load_host(functions):
+def _load_host(functions, int8_functions):
     """``_bcq_host``, bound to the library's functions: it holds torch's inline code and so fits one Python and one torch only."""
     try:
         from . import _bcq_host as host
@@ -48,6 +50,7 @@ def _load_host(functions):
                       "(`python paper_2510_10467_amd/build.py`)", RuntimeWarning, stacklevel=3)
         return _NoHost
     host.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in functions), BcqError)
+    host.bind_int8(*(ctypes.cast(f, ctypes.c_void_p).value for f in int8_functions))
     return host
 
 
@@ -94,7 +97,17 @@ def lib() -> ctypes.CDLL:
         for f in (L.bcq_select_kernel, L.bcq_pack, L.bcq_unpack, L.bcq_gemv, L.bcq_gemm_mixed, L.bcq_gemv_offset,
                   L.bcq_gemm_mixed_offset):
             f.restype = i32
-        _host = _load_host((L.bcq_gemv_offset, L.bcq_gemv_multi, L.bcq_gemm_mixed, L.bcq_gemm_mixed_offset))
+        L.bcq_int8_quantize.argtypes = [vp, i32, vp, vp, i64, i64, vp]
+        L.bcq_int8_gemm.argtypes = [vp, vp, vp, vp, vp, i32, i64, i64, i64, vp]
+        L.bcq_int8_gated.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, i32, i64, i64, i64, vp]
+        L.bcq_int8_backward_workspace.argtypes = [i32, i64, i64]
+        L.bcq_int8_backward_workspace.restype = i64
+        L.bcq_int8_gemm_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i64, i64, i64, vp, i64, vp]
+        L.bcq_int8_gated_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, i32, i64, i64, i64, vp, i64, vp]
+        for f in (L.bcq_int8_quantize, L.bcq_int8_gemm, L.bcq_int8_gated, L.bcq_int8_gemm_backward, L.bcq_int8_gated_backward):
+            f.restype = i32
+        _host = _load_host((L.bcq_gemv_offset, L.bcq_gemv_multi, L.bcq_gemm_mixed, L.bcq_gemm_mixed_offset),
+                           (L.bcq_int8_quantize, L.bcq_int8_gemm, L.bcq_int8_gated))
         _lib = L
     return _lib
 
@@ -318,6 +331,152 @@ def bcq_quantize(w: torch.Tensor, p_low: int, p_high: int, cycles: int, group: i
                                    ctypes.cast(op, ctypes.c_void_p) if offsets_by_p is not None else None,
                                    m, n, group, _stream()), "bcq_quantize")
     return planes, scales_by_p, offsets_by_p
+
+
+def _type(dtype, where: str) -> int:
+    if dtype not in TYPES:
+        raise TypeError(f"{where}: 16-bit tensors are torch.float16 or torch.bfloat16, got {dtype}")
+    return TYPES[dtype]
+
+
+def _activation(name, where: str) -> int:
+    if name not in ACTIVATIONS:
+        raise ValueError(f"{where}: activation must be one of {sorted(ACTIVATIONS)}, got {name!r}")
+    return ACTIVATIONS[name]
+
+
+def _int8_shapes(where: str, q, token_scales, mats) -> tuple:
+    """(tokens, m, n) of the codes of some tokens and of one or two matrices with their scales, all on one device."""
+    for t in (q, token_scales, *(t for pair in mats for t in pair)):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{where}: codes and scales must be GPU tensors (there is no CPU path)")
+        if t.device != q.device:
+            raise ValueError(f"{where}: tensors on several devices")
+    if q.dim() != 2 or token_scales.shape != q.shape[:1]:
+        raise ValueError(f"{where}: inconsistent shapes")
+    m, n = mats[0][0].shape[0], q.shape[1]
+    for w, c in mats:
+        if w.shape != (m, n) or c.shape != (m,):
+            raise ValueError(f"{where}: inconsistent shapes")
+    return q.shape[0], m, n
+
+
+def _int8_result(where: str, t, shape: tuple, dtype, like) -> torch.Tensor:
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    if not isinstance(t, torch.Tensor) or t.shape != shape or t.device != like.device:
+        raise ValueError(f"{where}: the result's tensor has the wrong shape or device")
+    return t
+
+
+def bcq_int8_quantize(x: torch.Tensor, q: torch.Tensor | None = None, scales: torch.Tensor | None = None) -> tuple:
+    """Rows of float16 or bfloat16 [rows][n] to ``(codes int8 [rows][n], scales float32 [rows])``: scale max |x| / 127, codes rounded to
+    nearest, ties to even.  Tokens at run time, output channels of a weight matrix offline."""
+    if _host is None:
+        lib()
+    done = _host.int8_quantize(x, q, scales)
+    if done is not None:
+        return done
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise TypeError("x must be a GPU tensor (there is no CPU path)")
+    if x.dim() != 2:
+        raise ValueError("bcq_int8_quantize: x must be [rows][n]")
+    rows, n = x.shape
+    kind = _type(x.dtype, "bcq_int8_quantize")
+    q = _int8_result("bcq_int8_quantize", q, (rows, n), torch.int8, x)
+    scales = _int8_result("bcq_int8_quantize", scales, (rows,), torch.float32, x)
+    with torch.cuda.device(x.device):
+        _check(lib().bcq_int8_quantize(_dev(x, x.dtype, "x"), kind, _dev(q, torch.int8, "q"), _dev(scales, torch.float32, "scales"), rows, n,
+                                       _stream()), "bcq_int8_quantize")
+    return q, scales
+
+
+def bcq_int8_gemm(q: torch.Tensor, token_scales: torch.Tensor, w: torch.Tensor, channel_scales: torch.Tensor,
+                  dtype: torch.dtype = torch.float16, y: torch.Tensor | None = None) -> torch.Tensor:
+    """y[t][r] = token_scales[t] * channel_scales[r] * sum_j q[t][j] w[r][j]: int8 codes q [tokens][n] and w [m][n], float32 scales,
+    y [tokens][m] of ``dtype`` (float16 or bfloat16; a given ``y`` must have it)."""
+    if _host is None:
+        lib()
+    done = _host.int8_gemm(q, token_scales, w, channel_scales, dtype, y)
+    if done is not None:
+        return done
+    tokens, m, n = _int8_shapes("bcq_int8_gemm", q, token_scales, [(w, channel_scales)])
+    kind = _type(dtype, "bcq_int8_gemm")
+    y = _int8_result("bcq_int8_gemm", y, (tokens, m), dtype, q)
+    with torch.cuda.device(q.device):
+        _check(lib().bcq_int8_gemm(_dev(q, torch.int8, "q"), _dev(token_scales, torch.float32, "token_scales"), _dev(w, torch.int8, "w"),
+                                   _dev(channel_scales, torch.float32, "channel_scales"), _dev(y, dtype, "y"), kind, m, n, tokens, _stream()),
+               "bcq_int8_gemm")
+    return y
+
+
+def bcq_int8_gated(q: torch.Tensor, token_scales: torch.Tensor, w_gate: torch.Tensor, gate_scales: torch.Tensor, w_up: torch.Tensor,
+                   up_scales: torch.Tensor, activation: str = "silu", dtype: torch.dtype = torch.float16,
+                   h: torch.Tensor | None = None) -> torch.Tensor:
+    """The gated feed-forward block up to its down projection in one kernel: h = act(g) * u with g and u the 8-bit products
+    (``bcq_int8_gemm``, not rounded) of the gate and up matrices.  ``activation``: "silu" or "gelu" (tanh form)."""
+    if _host is None:
+        lib()
+    done = _host.int8_gated(q, token_scales, w_gate, gate_scales, w_up, up_scales, activation, dtype, h)
+    if done is not None:
+        return done
+    tokens, m, n = _int8_shapes("bcq_int8_gated", q, token_scales, [(w_gate, gate_scales), (w_up, up_scales)])
+    kind, act = _type(dtype, "bcq_int8_gated"), _activation(activation, "bcq_int8_gated")
+    h = _int8_result("bcq_int8_gated", h, (tokens, m), dtype, q)
+    with torch.cuda.device(q.device):
+        _check(lib().bcq_int8_gated(_dev(q, torch.int8, "q"), _dev(token_scales, torch.float32, "token_scales"),
+                                    _dev(w_gate, torch.int8, "w_gate"), _dev(gate_scales, torch.float32, "gate_scales"),
+                                    _dev(w_up, torch.int8, "w_up"), _dev(up_scales, torch.float32, "up_scales"), act, _dev(h, dtype, "h"),
+                                    kind, m, n, tokens, _stream()), "bcq_int8_gated")
+    return h
+
+
+def _int8_backward_setup(where: str, dy, tokens: int, m: int, n: int, matrices: int, like) -> tuple:
+    """The type, dx and the workspace of a backward call."""
+    if not isinstance(dy, torch.Tensor) or not dy.is_cuda:
+        raise TypeError(f"{where}: the gradient must be a GPU tensor (there is no CPU path)")
+    if dy.shape != (tokens, m) or dy.device != like.device:
+        raise ValueError(f"{where}: the gradient has the wrong shape or device")
+    kind = _type(dy.dtype, where)
+    size = lib().bcq_int8_backward_workspace(matrices, m, tokens)
+    _check(min(size, 0), where)
+    return (kind, torch.empty((tokens, n), dtype=dy.dtype, device=like.device), size,
+            torch.empty((size,), dtype=torch.uint8, device=like.device))
+
+
+def bcq_int8_gemm_backward(dy: torch.Tensor, q: torch.Tensor, token_scales: torch.Tensor, w: torch.Tensor,
+                           channel_scales: torch.Tensor) -> tuple:
+    """Gradients of ``bcq_int8_gemm`` with the codes fixed: ``(dx [tokens][n] of dy's type, dchannel_scales float32 [m])``, dx being the
+    gradient of the activations that were quantised."""
+    where = "bcq_int8_gemm_backward"
+    lib()
+    tokens, m, n = _int8_shapes(where, q, token_scales, [(w, channel_scales)])
+    with torch.cuda.device(q.device):
+        kind, dx, size, workspace = _int8_backward_setup(where, dy, tokens, m, n, 1, q)
+        dscales = torch.empty((m,), dtype=torch.float32, device=q.device)
+        _check(lib().bcq_int8_gemm_backward(_dev(dy, dy.dtype, "dy"), _dev(q, torch.int8, "q"), _dev(token_scales, torch.float32, "token_scales"),
+                                            _dev(w, torch.int8, "w"), _dev(channel_scales, torch.float32, "channel_scales"), dx.data_ptr(),
+                                            dscales.data_ptr(), kind, m, n, tokens, workspace.data_ptr(), size, _stream()), where)
+    return dx, dscales
+
+
+def bcq_int8_gated_backward(dh: torch.Tensor, q: torch.Tensor, token_scales: torch.Tensor, w_gate: torch.Tensor, gate_scales: torch.Tensor,
+                            w_up: torch.Tensor, up_scales: torch.Tensor, activation: str = "silu") -> tuple:
+    """Gradients of ``bcq_int8_gated`` with the codes fixed: ``(dx [tokens][n] of dh's type, dgate_scales float32 [m], dup_scales float32
+    [m])``; the projections are computed again."""
+    where = "bcq_int8_gated_backward"
+    lib()
+    tokens, m, n = _int8_shapes(where, q, token_scales, [(w_gate, gate_scales), (w_up, up_scales)])
+    act = _activation(activation, where)
+    with torch.cuda.device(q.device):
+        kind, dx, size, workspace = _int8_backward_setup(where, dh, tokens, m, n, 2, q)
+        dgate, dup = (torch.empty((m,), dtype=torch.float32, device=q.device) for _ in range(2))
+        _check(lib().bcq_int8_gated_backward(_dev(dh, dh.dtype, "dh"), _dev(q, torch.int8, "q"),
+                                             _dev(token_scales, torch.float32, "token_scales"), _dev(w_gate, torch.int8, "w_gate"),
+                                             _dev(gate_scales, torch.float32, "gate_scales"), _dev(w_up, torch.int8, "w_up"),
+                                             _dev(up_scales, torch.float32, "up_scales"), act, dx.data_ptr(), dgate.data_ptr(),
+                                             dup.data_ptr(), kind, m, n, tokens, workspace.data_ptr(), size, _stream()), where)
+    return dx, dgate, dup
 
 
 def bench_stream_read(buf: torch.Tensor, sink: torch.Tensor) -> None:

@@ -8,6 +8,7 @@
 
 #include "bcq.h"
 #include "bcq_bench.h"
+#include "bcq_int8.hpp"
 #include "bcq_internal.hpp"
 
 namespace {
@@ -151,6 +152,63 @@ int run(const bcq::GemmArgs &a, hipStream_t stream)
     return err == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;
 }
 
+// 8-bit operators.  Row counts that keep tile numbers and byte offsets inside a tile in 32 bits.
+constexpr int64_t kInt8MaxRows = int64_t(1) << 24, kInt8MaxBackwardRows = int64_t(1) << 20;
+
+int check_int8(int type, int activation, int64_t m, int64_t n, int64_t tokens, int64_t max_m)
+{
+    if (type != BCQ_FLOAT16 && type != BCQ_BFLOAT16) return BCQ_ERR_BAD_TYPE;
+    if (activation != BCQ_ACT_SILU && activation != BCQ_ACT_GELU) return BCQ_ERR_BAD_TYPE;
+    // 128 * 128 * n stays below 2^31
+    if (m < 1 || m > max_m || n < 16 || n > 131056 || n % 16 != 0 || tokens < 0 || tokens > kInt8MaxRows || m * tokens > int64_t(1) << 40)
+        return BCQ_ERR_BAD_SHAPE;
+    return BCQ_OK;
+}
+
+bcq::Int8Args int8_args(const int8_t *q, const float *token_scales, const int8_t *w0, const float *c0, const int8_t *w1, const float *c1,
+                        int matrices, int activation, void *y, int type, int64_t m, int64_t n, int64_t tokens)
+{
+    bcq::Int8Args a{};
+    a.q = q;
+    a.token_scales = token_scales;
+    a.w[0] = w0;
+    a.w[1] = w1;
+    a.channel_scales[0] = c0;
+    a.channel_scales[1] = c1;
+    a.matrices = matrices;
+    a.activation = activation;
+    a.bf16 = type == BCQ_BFLOAT16;
+    a.y = static_cast<uint16_t *>(y);
+    a.m = m;
+    a.n = n;
+    a.tokens = tokens;
+    return a;
+}
+
+int run_int8(const bcq::Int8Args &a, void *stream)
+{
+    if (a.tokens == 0) return BCQ_OK;
+    const bool rows = bcq::int8_rows_supports(a);
+    const hipError_t err = rows ? bcq::int8_rows_launch(a, static_cast<hipStream_t>(stream)) : bcq::int8_tile_launch(a, static_cast<hipStream_t>(stream));
+    g_last = rows ? "int8_rows" : "int8_tile";
+    return err == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;
+}
+
+int run_int8_backward(bcq::Int8Args a, const void *dy, void *dx, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    if (!workspace) return BCQ_ERR_NULL;
+    if (!aligned(dy, 2) || !aligned(a.q, 16) || !aligned(a.token_scales, 4) || !aligned(dx, 16) || !aligned(a.dscales[0], 4) ||
+        !aligned(a.dscales[1], 4) || !aligned(workspace, 256))
+        return BCQ_ERR_ALIGN;
+    if (workspace_bytes < bcq::int8_workspace(a.matrices, a.m, a.tokens).bytes) return BCQ_ERR_WORKSPACE;
+    a.dy = static_cast<const uint16_t *>(dy);
+    a.dx = static_cast<uint16_t *>(dx);
+    a.workspace = workspace;
+    const hipError_t err = bcq::int8_backward_launch(a, static_cast<hipStream_t>(stream));
+    g_last = "int8_backward";
+    return err == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;
+}
+
 }  // namespace
 
 namespace bcq {
@@ -180,10 +238,12 @@ const char *bcq_strerror(int status)
     case BCQ_OK: return "ok";
     case BCQ_ERR_NULL: return "a required pointer is NULL";
     case BCQ_ERR_BAD_P: return "precision or plane count out of range";
-    case BCQ_ERR_BAD_SHAPE: return "shape violates m>=1, n>=group, group%32==0, n%group==0, batch>=0";
-    case BCQ_ERR_ALIGN: return "pointer not aligned (planes/scales/x: 16 bytes, y: 2 bytes)";
+    case BCQ_ERR_BAD_SHAPE: return "shape violates m>=1, n>=group, group%32==0, n%group==0, batch>=0 (8-bit operators: m, n, tokens in range, n%16==0)";
+    case BCQ_ERR_ALIGN: return "pointer not aligned (planes/scales/x: 16 bytes, y: 2 bytes; 8-bit operators: codes/x/dx: 16, float scales: 4, workspace: 256)";
     case BCQ_ERR_HIP: return "HIP runtime error at kernel launch";
     case BCQ_ERR_VARIANT: return "forced kernel variant unknown or unable to run this problem";
+    case BCQ_ERR_BAD_TYPE: return "type or activation out of range";
+    case BCQ_ERR_WORKSPACE: return "workspace smaller than bcq_int8_backward_workspace says";
     default: return "unknown status";
     }
 }
@@ -415,6 +475,71 @@ int bcq_quantize_form(const bcq_half *w, int p_low, int p_high, int cycles, int 
                                           residual_form == BCQ_RESIDUAL_LISTING, static_cast<hipStream_t>(stream));
     g_last = "quantize";
     return err == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;
+}
+
+int bcq_int8_quantize(const void *x, int type, int8_t *q, float *scales, int64_t rows, int64_t n, void *stream)
+{
+    if (int rc = check_int8(type, BCQ_ACT_SILU, 1, n, rows, kInt8MaxRows)) return rc;
+    if (rows == 0) return BCQ_OK;
+    if (!x || !q || !scales) return BCQ_ERR_NULL;
+    if (!aligned(x, 16) || !aligned(q, 16) || !aligned(scales, 4)) return BCQ_ERR_ALIGN;
+    const hipError_t err = bcq::int8_quantize_launch(static_cast<const uint16_t *>(x), type == BCQ_BFLOAT16, q, scales, rows, n,
+                                                     static_cast<hipStream_t>(stream));
+    g_last = "int8_quantize";
+    return err == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;
+}
+
+int bcq_int8_gemm(const int8_t *q, const float *token_scales, const int8_t *w, const float *channel_scales, void *y, int type,
+                  int64_t m, int64_t n, int64_t tokens, void *stream)
+{
+    if (int rc = check_int8(type, BCQ_ACT_SILU, m, n, tokens, kInt8MaxRows)) return rc;
+    if (!w || !channel_scales || (tokens > 0 && (!q || !token_scales || !y))) return BCQ_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(token_scales, 4) || !aligned(w, 16) || !aligned(channel_scales, 4) || !aligned(y, 2)) return BCQ_ERR_ALIGN;
+    return run_int8(int8_args(q, token_scales, w, channel_scales, w, channel_scales, 1, BCQ_ACT_SILU, y, type, m, n, tokens), stream);
+}
+
+int bcq_int8_gated(const int8_t *q, const float *token_scales, const int8_t *w_gate, const float *gate_scales, const int8_t *w_up,
+                   const float *up_scales, int activation, void *h, int type, int64_t m, int64_t n, int64_t tokens, void *stream)
+{
+    if (int rc = check_int8(type, activation, m, n, tokens, kInt8MaxRows)) return rc;
+    if (!w_gate || !gate_scales || !w_up || !up_scales || (tokens > 0 && (!q || !token_scales || !h))) return BCQ_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(token_scales, 4) || !aligned(w_gate, 16) || !aligned(w_up, 16) || !aligned(gate_scales, 4) ||
+        !aligned(up_scales, 4) || !aligned(h, 2))
+        return BCQ_ERR_ALIGN;
+    return run_int8(int8_args(q, token_scales, w_gate, gate_scales, w_up, up_scales, 2, activation, h, type, m, n, tokens), stream);
+}
+
+int64_t bcq_int8_backward_workspace(int matrices, int64_t m, int64_t tokens)
+{
+    if (matrices < 1 || matrices > 2) return BCQ_ERR_BAD_SHAPE;
+    if (int rc = check_int8(BCQ_FLOAT16, BCQ_ACT_SILU, m, 16, tokens, kInt8MaxBackwardRows)) return rc;
+    return bcq::int8_workspace(matrices, m, tokens).bytes;
+}
+
+int bcq_int8_gemm_backward(const void *dy, const int8_t *q, const float *token_scales, const int8_t *w, const float *channel_scales,
+                           void *dx, float *dchannel_scales, int type, int64_t m, int64_t n, int64_t tokens, void *workspace,
+                           int64_t workspace_bytes, void *stream)
+{
+    if (int rc = check_int8(type, BCQ_ACT_SILU, m, n, tokens, kInt8MaxBackwardRows)) return rc;
+    if (!w || !channel_scales || !dchannel_scales || (tokens > 0 && (!dy || !q || !token_scales || !dx))) return BCQ_ERR_NULL;
+    if (!aligned(w, 16) || !aligned(channel_scales, 4)) return BCQ_ERR_ALIGN;
+    bcq::Int8Args a = int8_args(q, token_scales, w, channel_scales, w, channel_scales, 1, BCQ_ACT_SILU, nullptr, type, m, n, tokens);
+    a.dscales[0] = a.dscales[1] = dchannel_scales;
+    return run_int8_backward(a, dy, dx, workspace, workspace_bytes, stream);
+}
+
+int bcq_int8_gated_backward(const void *dh, const int8_t *q, const float *token_scales, const int8_t *w_gate, const float *gate_scales,
+                            const int8_t *w_up, const float *up_scales, int activation, void *dx, float *dgate_scales, float *dup_scales,
+                            int type, int64_t m, int64_t n, int64_t tokens, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    if (int rc = check_int8(type, activation, m, n, tokens, kInt8MaxBackwardRows)) return rc;
+    if (!w_gate || !gate_scales || !w_up || !up_scales || !dgate_scales || !dup_scales || (tokens > 0 && (!dh || !q || !token_scales || !dx)))
+        return BCQ_ERR_NULL;
+    if (!aligned(w_gate, 16) || !aligned(w_up, 16) || !aligned(gate_scales, 4) || !aligned(up_scales, 4)) return BCQ_ERR_ALIGN;
+    bcq::Int8Args a = int8_args(q, token_scales, w_gate, gate_scales, w_up, up_scales, 2, activation, nullptr, type, m, n, tokens);
+    a.dscales[0] = dgate_scales;
+    a.dscales[1] = dup_scales;
+    return run_int8_backward(a, dh, dx, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -12,6 +12,7 @@
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/ops/empty.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "bcq.h"
@@ -22,6 +23,9 @@ decltype(&bcq_gemv_offset) g_gemv = nullptr;
 decltype(&bcq_gemv_multi) g_multi = nullptr;
 decltype(&bcq_gemm_mixed) g_mixed = nullptr;
 decltype(&bcq_gemm_mixed_offset) g_mixed_offset = nullptr;
+decltype(&bcq_int8_quantize) g_int8_quantize = nullptr;
+decltype(&bcq_int8_gemm) g_int8_gemm = nullptr;
+decltype(&bcq_int8_gated) g_int8_gated = nullptr;
 PyObject *g_error = nullptr;            // the exception class: (status, where)
 
 // A plain tensor on the GPU, contiguous, of this type; nullptr otherwise.  (Subclasses, wrappers and tensors without storage go the Python way.)
@@ -52,10 +56,10 @@ struct WithoutGil {
     ~WithoutGil() { PyEval_RestoreThread(state); }
 };
 
-at::Tensor output(const at::Tensor &x, int64_t batch, int64_t m)
+at::Tensor output(const at::Tensor &x, at::IntArrayRef sizes, at::ScalarType type)
 {
     WithoutGil released;
-    return at::empty({batch, m}, at::TensorOptions().dtype(at::kHalf).device(x.device()));
+    return at::empty(sizes, at::TensorOptions().dtype(type).device(x.device()));
 }
 
 template <typename F, typename... Args>
@@ -100,7 +104,7 @@ const bcq_half *half(const at::Tensor *t) { return static_cast<const bcq_half *>
 PyObject *result(PyObject *given, const at::Tensor &x, int64_t batch, int64_t m, bcq_half *&ptr)
 {
     if (given == Py_None) {
-        at::Tensor y = output(x, batch, m);
+        at::Tensor y = output(x, {batch, m}, at::kHalf);
         ptr = static_cast<bcq_half *>(y.mutable_data_ptr());
         return THPVariable_Wrap(std::move(y));
     }
@@ -240,6 +244,145 @@ PyObject *gemm_mixed(PyObject *, PyObject *const *a, Py_ssize_t count)
     });
 }
 
+// A 16-bit type by its torch name; false otherwise.
+bool type_of(at::ScalarType scalar, int &type)
+{
+    if (scalar != at::kHalf && scalar != at::kBFloat16) return false;
+    type = scalar == at::kHalf ? BCQ_FLOAT16 : BCQ_BFLOAT16;
+    return true;
+}
+
+// Tensors of the 8-bit operators live on one device, the current one.
+struct OneDevice {
+    c10::Device device;
+    bool same = true;
+    explicit OneDevice(const at::Tensor &first) : device(first.device()) { same = device.index() == c10::hip::current_device(); }
+    const at::Tensor *take(PyObject *o, at::ScalarType type)
+    {
+        const at::Tensor *t = gpu_tensor(o, type);
+        if (t && t->device() != device) t = nullptr;
+        if (!t) same = false;
+        return t;
+    }
+    // [rows] or [rows][cols], the caller's or a new one; nullptr where the caller's does not fit
+    PyObject *result(PyObject *given, const at::Tensor &like, at::ScalarType type, at::IntArrayRef sizes, void *&ptr)
+    {
+        if (given == Py_None) {
+            at::Tensor y = output(like, sizes, type);
+            ptr = y.mutable_data_ptr();
+            return THPVariable_Wrap(std::move(y));
+        }
+        const at::Tensor *y = take(given, type);
+        if (!y || y->sizes() != sizes) return nullptr;
+        ptr = y->mutable_data_ptr();
+        Py_INCREF(given);
+        return given;
+    }
+};
+
+// int8_quantize(x, q, scales) -> (codes, scales)
+PyObject *int8_quantize(PyObject *, PyObject *const *a, Py_ssize_t count)
+{
+    if (count != 3 || !g_int8_quantize) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *x = gpu_tensor(a[0], at::kHalf);
+        if (!x) x = gpu_tensor(a[0], at::kBFloat16);
+        int type;
+        if (!x || x->dim() != 2 || !type_of(x->scalar_type(), type)) Py_RETURN_NONE;
+        OneDevice on(*x);
+        if (!on.same) Py_RETURN_NONE;
+        const int64_t rows = x->size(0), n = x->size(1);
+        void *q_to = nullptr, *s_to = nullptr;
+        PyObject *q = on.result(a[1], *x, at::kChar, {rows, n}, q_to);
+        if (!q) Py_RETURN_NONE;
+        PyObject *s = nullptr;
+        try {
+            s = on.result(a[2], *x, at::kFloat, {rows}, s_to);
+        } catch (...) {
+        }
+        PyObject *both = s ? PyTuple_New(2) : nullptr;
+        if (!both) {
+            PyErr_Clear();
+            Py_DECREF(q);
+            Py_XDECREF(s);
+            Py_RETURN_NONE;
+        }
+        PyTuple_SET_ITEM(both, 0, q);
+        PyTuple_SET_ITEM(both, 1, s);
+        return finish(launch(g_int8_quantize, x->const_data_ptr(), type, static_cast<int8_t *>(q_to), static_cast<float *>(s_to), rows, n, stream()),
+                      "bcq_int8_quantize", both);
+    });
+}
+
+const int8_t *codes(const at::Tensor *t) { return static_cast<const int8_t *>(t->const_data_ptr()); }
+const float *floats(const at::Tensor *t) { return static_cast<const float *>(t->const_data_ptr()); }
+
+// The codes of some tokens and `mats` matrices, each with its scales: a[0], a[1], then pairs.  False where they do not fit together.
+bool int8_operands(OneDevice &on, PyObject *const *a, int mats, const at::Tensor **t, int64_t &m, int64_t &n, int64_t &tokens)
+{
+    for (int k = 0; k < 2 + 2 * mats; ++k)
+        if (!(t[k] = on.take(a[k], k & 1 ? at::kFloat : at::kChar))) return false;
+    if (t[0]->dim() != 2 || t[2]->dim() != 2) return false;
+    tokens = t[0]->size(0);
+    n = t[0]->size(1);
+    m = t[2]->size(0);
+    if (t[1]->dim() != 1 || t[1]->size(0) != tokens) return false;
+    for (int k = 2; k < 2 + 2 * mats; k += 2)
+        if (!matrix_fits(t[k], m, n) || t[k + 1]->dim() != 1 || t[k + 1]->size(0) != m) return false;
+    return on.same;
+}
+
+// int8_gemm(q, token_scales, w, channel_scales, dtype, y)
+PyObject *int8_gemm(PyObject *, PyObject *const *a, Py_ssize_t count)
+{
+    if (count != 6 || !g_int8_gemm) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject * {
+        int type;
+        const at::Tensor *q = gpu_tensor(a[0], at::kChar), *t[4];
+        if (!q || !THPDtype_Check(a[4]) || !type_of(reinterpret_cast<THPDtype *>(a[4])->scalar_type, type)) Py_RETURN_NONE;
+        OneDevice on(*q);
+        int64_t m, n, tokens;
+        if (!int8_operands(on, a, 1, t, m, n, tokens)) Py_RETURN_NONE;
+        void *to = nullptr;
+        PyObject *y = on.result(a[5], *q, type == BCQ_FLOAT16 ? at::kHalf : at::kBFloat16, {tokens, m}, to);
+        if (!y) Py_RETURN_NONE;
+        return finish(launch(g_int8_gemm, codes(t[0]), floats(t[1]), codes(t[2]), floats(t[3]), to, type, m, n, tokens, stream()), "bcq_int8_gemm", y);
+    });
+}
+
+// int8_gated(q, token_scales, w_gate, gate_scales, w_up, up_scales, activation, dtype, h)
+PyObject *int8_gated(PyObject *, PyObject *const *a, Py_ssize_t count)
+{
+    if (count != 9 || !g_int8_gated) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject * {
+        int type;
+        const at::Tensor *q = gpu_tensor(a[0], at::kChar), *t[6];
+        if (!q || !PyUnicode_CheckExact(a[6]) || !THPDtype_Check(a[7]) || !type_of(reinterpret_cast<THPDtype *>(a[7])->scalar_type, type)) Py_RETURN_NONE;
+        const bool silu = PyUnicode_CompareWithASCIIString(a[6], "silu") == 0;
+        if (!silu && PyUnicode_CompareWithASCIIString(a[6], "gelu") != 0) Py_RETURN_NONE;
+        OneDevice on(*q);
+        int64_t m, n, tokens;
+        if (!int8_operands(on, a, 2, t, m, n, tokens)) Py_RETURN_NONE;
+        void *to = nullptr;
+        PyObject *h = on.result(a[8], *q, type == BCQ_FLOAT16 ? at::kHalf : at::kBFloat16, {tokens, m}, to);
+        if (!h) Py_RETURN_NONE;
+        return finish(launch(g_int8_gated, codes(t[0]), floats(t[1]), codes(t[2]), floats(t[3]), codes(t[4]), floats(t[5]),
+                             (int)(silu ? BCQ_ACT_SILU : BCQ_ACT_GELU), to, type, m, n, tokens, stream()),
+                      "bcq_int8_gated", h);
+    });
+}
+
+// bind_int8(quantize, gemm, gated): likewise the 8-bit operators
+PyObject *bind_int8(PyObject *, PyObject *args)
+{
+    unsigned long long f[3];
+    if (!PyArg_ParseTuple(args, "KKK", &f[0], &f[1], &f[2])) return nullptr;
+    g_int8_quantize = reinterpret_cast<decltype(g_int8_quantize)>(f[0]);
+    g_int8_gemm = reinterpret_cast<decltype(g_int8_gemm)>(f[1]);
+    g_int8_gated = reinterpret_cast<decltype(g_int8_gated)>(f[2]);
+    Py_RETURN_NONE;
+}
+
 // bind(gemv_offset, gemv_multi, gemm_mixed, gemm_mixed_offset, error): addresses of the C ABI's functions in the library that is loaded
 PyObject *bind(PyObject *, PyObject *args)
 {
@@ -258,7 +401,11 @@ PyObject *bind(PyObject *, PyObject *args)
 PyMethodDef g_methods[] = {{"gemv", (PyCFunction)(void (*)(void))gemv, METH_FASTCALL, nullptr},
                            {"gemv_multi", (PyCFunction)(void (*)(void))gemv_multi, METH_FASTCALL, nullptr},
                            {"gemm_mixed", (PyCFunction)(void (*)(void))gemm_mixed, METH_FASTCALL, nullptr},
+                           {"int8_quantize", (PyCFunction)(void (*)(void))int8_quantize, METH_FASTCALL, nullptr},
+                           {"int8_gemm", (PyCFunction)(void (*)(void))int8_gemm, METH_FASTCALL, nullptr},
+                           {"int8_gated", (PyCFunction)(void (*)(void))int8_gated, METH_FASTCALL, nullptr},
                            {"bind", bind, METH_VARARGS, nullptr},
+                           {"bind_int8", bind_int8, METH_VARARGS, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_bcq_host", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

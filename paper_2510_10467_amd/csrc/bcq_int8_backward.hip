@@ -1,0 +1,290 @@
+// The backward passes of the 8-bit products, codes fixed: gradients of the activations and of the channel scales.
+//
+//   norms     per token the power of two f_t that brings its largest |dy| to [1/32, 1/16), and the power of two above all channel scales, S
+//   first     (bcq_int8_tile.hip) G = binary16 of f_t dg c / S for every channel of every matrix, and partial sums of dc
+//   sums      dc: the partial sums of a channel, in order
+//   second    dx = (S / f_t) sum over channels of G w: a product over the weights' ROWS
+//
+// The second product runs on v_mfma_f32_32x32x16_f16.  Both operands go into LDS by loads that write there, the weights as they are stored: 64
+// rows of 8-bit codes by a tile's columns.  A lane needs eight codes of one column, which is what the transposing LDS read of
+// 8-bit values delivers (16 lanes take eight rows of 16 columns), and turns them into binary16, exactly: a code's byte
+// with its sign bit turned under the byte 0x64 is the number 1024 + 128 + code.
+#include "bcq_int8.hpp"
+#include "bcq_internal.hpp"
+
+namespace bcq {
+namespace {
+
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef int v2i __attribute__((ext_vector_type(2)));
+
+// One workgroup per token, and a last one for the scales.
+__global__ __launch_bounds__(256) void int8_norms_kernel(const uint16_t *__restrict__ dy, const float *__restrict__ c0, const float *__restrict__ c1,
+                                                         float *__restrict__ norms, float *__restrict__ scale_top, int64_t m, int64_t tokens, bool bf16,
+                                                         bool whole)
+{
+    __shared__ float tops[4];
+    float top = 0.f;                                    // (a NaN leaves it as it is: such a token's results are NaN whatever its power)
+    const int64_t token = blockIdx.x;
+    if (token < tokens) {
+        const uint16_t *row = dy + token * m;
+        if (whole) {
+            for (int64_t j = threadIdx.x; j * 8 < m; j += 256) {
+                const u32x4 v = *reinterpret_cast<const u32x4 *>(row + j * 8);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(from_16(v[i] & 0xffffu, bf16)), fabsf(from_16(v[i] >> 16, bf16))));
+            }
+        } else {
+            for (int64_t j = threadIdx.x; j < m; j += 256) top = fmaxf(top, fabsf(from_16(row[j], bf16)));
+        }
+    } else {
+        for (int64_t j = threadIdx.x; j < m; j += 256) top = fmaxf(top, fmaxf(fabsf(c0[j]), fabsf(c1[j])));
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    const bool usable = top > 0.f && top < __builtin_inff();
+    const int e = usable ? min(max(ilogbf(top), -120), 120) : 0;
+    if (token < tokens) norms[token] = ldexpf(1.f, usable ? -5 - e : 0);
+    else *scale_top = ldexpf(1.f, usable ? e + 1 : 0);
+}
+
+__global__ __launch_bounds__(256) void int8_sums_kernel(const float *__restrict__ parts, float *__restrict__ d0, float *__restrict__ d1, int64_t m,
+                                                        int matrices, int64_t part_count)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= m * matrices) return;
+    float sum = 0.f;
+    for (int64_t p = 0; p < part_count; ++p) sum += parts[p * m * matrices + i];
+    if (i < m) d0[i] = sum;
+    else d1[i - m] = sum;
+}
+
+struct SecondParams {
+    const _Float16 *grad;
+    const int8_t *w[2];
+    const float *norms, *scale_top;
+    uint16_t *dx;
+    uint32_t m, m_padded, n, tokens, grad_stride;
+    uint32_t column_tiles, token_tiles;
+    int matrices;
+    bool bf16, whole;
+};
+
+template <int WC_, int WT_, int FC_, int FT_>
+struct SecondShape {
+    static constexpr int WC = WC_, WT = WT_, FC = FC_, FT = FT_;
+    static constexpr int COLS = WC * FC * 32, TOKS = WT * FT * 32, WAVES = WC * WT;
+    static constexpr int W_BYTES = 64 * COLS, STAGE = W_BYTES + TOKS * 128;
+    static constexpr int OUT_ROW = COLS * 2 + 16, OUT = TOKS * OUT_ROW;
+    static constexpr int BYTES = 2 * STAGE > OUT ? 2 * STAGE : OUT;
+};
+
+// Eight codes to binary16: 1024 + (code + 128), less 1152.
+__device__ __forceinline__ v8h halves_of(v2i codes)
+{
+    u32x4 out;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const uint32_t c = (uint32_t)codes[k] ^ 0x80808080u;
+        const v2h bias = {(_Float16)1152.f, (_Float16)1152.f};
+        out[2 * k] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, __builtin_amdgcn_perm(0x64646464u, c, 0x04010400u)) - bias);
+        out[2 * k + 1] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, __builtin_amdgcn_perm(0x64646464u, c, 0x04030402u)) - bias);
+    }
+    return __builtin_bit_cast(v8h, out);
+}
+
+// A step is 64 rows of the weights: an LDS row holds COLS codes, its 16-byte parts XOR-permuted by the row's number; a token's 64
+// gradients are a row of 128 bytes, permuted as in the first half.
+template <typename S>
+__global__ __launch_bounds__(S::WAVES * 64) void int8_second_kernel(const SecondParams a)
+{
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wc = wave / S::WT, wt = wave % S::WT;
+    const int r32 = lane & 31, half = lane >> 5;
+
+    const uint32_t total = gridDim.x, xcd = blockIdx.x & 7;
+    const uint32_t id = xcd * (total >> 3) + min(xcd, total & 7) + (blockIdx.x >> 3);
+    const uint32_t group = id / (8 * a.column_tiles);
+    const uint32_t in_group = min(8u, a.token_tiles - group * 8);
+    const uint32_t rest = id - group * 8 * a.column_tiles;
+    const uint32_t c0 = rest / in_group * S::COLS, t0 = (group * 8 + rest % in_group) * S::TOKS;
+    const uint32_t cols = min((uint32_t)S::COLS, a.n - c0), toks = min((uint32_t)S::TOKS, a.tokens - t0);
+
+    constexpr int W_LOADS = S::W_BYTES / 1024 / S::WAVES, G_LOADS = S::TOKS / 8 / S::WAVES;
+    constexpr int PARTS = S::COLS / 16, ROWS_PER = 64 / PARTS;          // parts of an LDS row, rows of a load
+    static_assert(W_LOADS * 1024 * S::WAVES == S::W_BYTES && G_LOADS * 8 * S::WAVES == S::TOKS, "whole loads per wave");
+    uint32_t g_src[G_LOADS];
+#pragma unroll
+    for (int k = 0; k < G_LOADS; ++k) {
+        const uint32_t tok = 8 * (wave * G_LOADS + k) + (lane >> 3);
+        g_src[k] = min(tok, toks - 1) * a.grad_stride * 2 + ((lane & 7) ^ ((tok >> 1) & 7)) * 16;
+    }
+    // load k of the weights: rows ROWS_PER * unit .. of the step, place lane % PARTS (columns past the end bring the last part)
+    uint32_t w_row[W_LOADS], w_col[W_LOADS];
+#pragma unroll
+    for (int k = 0; k < W_LOADS; ++k) {
+        w_row[k] = (wave * W_LOADS + k) * ROWS_PER + lane / PARTS;
+        w_col[k] = min((uint32_t)((lane % PARTS) ^ (w_row[k] & (PARTS - 1))) * 16, cols - 16);
+    }
+    const auto g_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16 *>(a.grad + (int64_t)t0 * a.grad_stride), 0,
+                                                          (int)(toks * a.grad_stride * 2), 0x00020000);
+    const uint32_t per_matrix = a.m_padded / 64;
+    const int steps = (int)(per_matrix * a.matrices);
+    // Rows past a matrix's end repeat its last one: the gradients there are zeros.
+    auto stage = [&](int buffer, uint32_t s) {
+        unsigned char *to = lds + buffer * S::STAGE;
+        const uint32_t k = s >= per_matrix ? 1 : 0, row0 = (s - k * per_matrix) * 64;
+        const uint32_t rows = min(64u, a.m - row0);
+        const auto w_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>((k ? a.w[1] : a.w[0]) + (int64_t)row0 * a.n + c0), 0,
+                                                              (int)((rows - 1) * a.n + cols), 0x00020000);
+#pragma unroll
+        for (int j = 0; j < W_LOADS; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(w_rsrc, (__attribute__((address_space(3))) void *)(to + (wave * W_LOADS + j) * 1024), 16,
+                                                     (int)(min(w_row[j], rows - 1) * a.n + w_col[j]), 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < G_LOADS; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(g_rsrc, (__attribute__((address_space(3))) void *)(to + S::W_BYTES + (wave * G_LOADS + j) * 1024), 16,
+                                                     (int)g_src[j], (int)(s * 128), 0, 0);
+    };
+
+    v16f acc[S::FC][S::FT];
+#pragma unroll
+    for (int c = 0; c < S::FC; ++c)
+#pragma unroll
+        for (int t = 0; t < S::FT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[c][t][i] = 0.f;
+
+    const uint32_t swz = (r32 >> 1) & 7;
+    // the transposing read: lanes 2 r and 2 r + 1 of sixteen point at the halves of row r's 16 columns; lanes 0-31 take rows 0-7 of a
+    // step of 16, lanes 32-63 rows 8-15, of which every second sixteen the next 16 columns
+    const int tr_row = half * 8 + ((lane & 15) >> 1);
+    auto multiply = [&](int buffer, int kk) {
+        const unsigned char *from = lds + buffer * S::STAGE;
+        v8h w[S::FC], g[S::FT];
+#pragma unroll
+        for (int c = 0; c < S::FC; ++c) {
+            const int row = kk * 16 + tr_row;
+            const int part = (wc * S::FC + c) * 2 + ((lane >> 4) & 1);
+            const unsigned char *at = from + row * S::COLS + ((part ^ (row & (PARTS - 1))) << 4) + (lane & 1) * 8;
+            w[c] = halves_of(__builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i *)at));
+        }
+#pragma unroll
+        for (int t = 0; t < S::FT; ++t)
+            g[t] = *reinterpret_cast<const v8h *>(from + S::W_BYTES + ((wt * S::FT + t) * 32 + r32) * 128 + (((2 * kk + half) ^ swz) << 4));
+#pragma unroll
+        for (int c = 0; c < S::FC; ++c)
+#pragma unroll
+            for (int t = 0; t < S::FT; ++t) acc[c][t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w[c], g[t], acc[c][t], 0, 0, 0);
+    };
+
+    stage(0, 0);
+    for (int s = 0; s < steps; ++s) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (s + 1 < steps) stage((s + 1) & 1, (uint32_t)(s + 1));
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) multiply(s & 1, kk);
+    }
+    __syncthreads();
+
+    const float top = *a.scale_top;
+#pragma unroll
+    for (int t = 0; t < S::FT; ++t) {
+        const uint32_t tok = (wt * S::FT + t) * 32 + r32;
+        const float back = 1.f / a.norms[t0 + min(tok, toks - 1)];      // (a power of two)
+#pragma unroll
+        for (int c = 0; c < S::FC; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int col = (wc * S::FC + c) * 32 + 8 * e + 4 * half;
+                uint32_t out[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) out[i] = to_16(acc[c][t][4 * e + i] * top * back, a.bf16);
+                *reinterpret_cast<u32x2 *>(lds + tok * S::OUT_ROW + col * 2) = u32x2{out[0] | out[1] << 16, out[2] | out[3] << 16};
+            }
+    }
+    __syncthreads();
+    constexpr int PIECES = S::COLS / 8;
+    for (int i = threadIdx.x; i < S::TOKS * PIECES; i += S::WAVES * 64) {
+        const uint32_t tok = i / PIECES, piece = i % PIECES;
+        if (tok < toks && piece * 8 < cols)
+            *reinterpret_cast<u32x4 *>(a.dx + (int64_t)(t0 + tok) * a.n + c0 + piece * 8) = *reinterpret_cast<const u32x4 *>(lds + tok * S::OUT_ROW + piece * 16);
+    }
+}
+
+template <typename S>
+hipError_t go(SecondParams p, hipStream_t stream)
+{
+    p.column_tiles = (p.n + S::COLS - 1) / S::COLS;
+    p.token_tiles = (p.tokens + S::TOKS - 1) / S::TOKS;
+    const auto kernel = int8_second_kernel<S>;
+    if (hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), S::BYTES)) return e;
+    hipLaunchKernelGGL(kernel, dim3(p.column_tiles * p.token_tiles), dim3(S::WAVES * 64), S::BYTES, stream, p);
+    return hipGetLastError();
+}
+
+using Large = SecondShape<4, 2, 2, 4>;      // 256 columns x 256 tokens
+using Medium = SecondShape<2, 2, 2, 2>;     // 128 x 128
+using Small = SecondShape<2, 2, 1, 1>;      // 64 x 64
+
+}  // namespace
+
+Int8Workspace int8_workspace(int matrices, int64_t m, int64_t tokens)
+{
+    Int8Workspace ws;
+    auto up = [](int64_t bytes) { return (bytes + 255) / 256 * 256; };
+    ws.grad_stride = matrices * ((m + 63) / 64 * 64);
+    ws.part_count = (tokens + 63) / 64 * 2 + 2;             // at most: a wave's tokens are 64, or 32 in tiles of 64
+    ws.grad = 0;
+    ws.norms = up(tokens * ws.grad_stride * 2);
+    ws.scale_top = ws.norms + up(tokens * 4);
+    ws.parts = ws.scale_top + 256;
+    ws.bytes = ws.parts + up(ws.part_count * matrices * m * 4);
+    return ws;
+}
+
+hipError_t int8_backward_launch(const Int8Args &a, hipStream_t stream)
+{
+    const Int8Workspace ws = int8_workspace(a.matrices, a.m, a.tokens);
+    unsigned char *base = static_cast<unsigned char *>(a.workspace);
+    float *norms = reinterpret_cast<float *>(base + ws.norms), *scale_top = reinterpret_cast<float *>(base + ws.scale_top);
+    int64_t part_count = 0;
+    if (a.tokens > 0) {
+        const bool whole = a.m % 8 == 0 && (reinterpret_cast<uintptr_t>(a.dy) & 15) == 0;
+        hipLaunchKernelGGL(int8_norms_kernel, dim3((unsigned)(a.tokens + 1)), dim3(256), 0, stream, a.dy, a.channel_scales[0],
+                           a.channel_scales[a.matrices - 1], norms, scale_top, a.m, a.tokens, a.bf16, whole);
+        if (hipError_t e = hipGetLastError()) return e;
+        if (hipError_t e = int8_tile_backward_launch(a, ws, stream, part_count)) return e;
+    }
+    hipLaunchKernelGGL(int8_sums_kernel, dim3((unsigned)((a.m * a.matrices + 255) / 256)), dim3(256), 0, stream,
+                       reinterpret_cast<const float *>(base + ws.parts), a.dscales[0], a.dscales[a.matrices - 1], a.m, a.matrices, part_count);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (a.tokens == 0) return hipSuccess;
+    SecondParams p{};
+    p.grad = reinterpret_cast<const _Float16 *>(base + ws.grad);
+    p.w[0] = a.w[0];
+    p.w[1] = a.w[a.matrices - 1];
+    p.norms = norms;
+    p.scale_top = scale_top;
+    p.dx = a.dx;
+    p.m = (uint32_t)a.m;
+    p.m_padded = (uint32_t)(ws.grad_stride / a.matrices);
+    p.n = (uint32_t)a.n;
+    p.tokens = (uint32_t)a.tokens;
+    p.grad_stride = (uint32_t)ws.grad_stride;
+    p.matrices = a.matrices;
+    p.bf16 = a.bf16;
+    auto tiles = [&](int64_t c, int64_t t) { return ((a.n + c - 1) / c) * ((a.tokens + t - 1) / t); };
+    if (tiles(256, 256) >= 256) return go<Large>(p, stream);
+    if (tiles(128, 128) >= 256) return go<Medium>(p, stream);
+    return go<Small>(p, stream);
+}
+
+}  // namespace bcq
