@@ -1,13 +1,19 @@
-// 8-bit products for few tokens.  The weights are read once, straight into the operand registers of
-// v_mfma_i32_16x16x64_i8 (a lane holds 16 bytes of row lane % 16), and the matrix instruction does the sum over columns: there is no
-// reduction across lanes, and the 16 columns of its result are 16 tokens, of which one costs no more than sixteen.
+// 8-bit products for few tokens: every wave streams rows of weights of its own through LDS of its own.
 //
-// A workgroup owns 16 BLOCKS rows (of gate and of up, where there are two) and all tokens; its waves take equal runs of 64-column steps, so
-// that a row's bytes are under way at once, and meet in LDS: sums of integers, in any order the same.  The codes of the
-// tokens come from the cache into registers beside the weights.
+// A workgroup owns 16 BLOCKS rows (of gate and of up, where there are two) and all tokens; its waves take equal runs of 128-column steps and meet at
+// the end in LDS, with sums of integers, which are the same in any order.  In between they share nothing and wait for nothing but their own loads.
+//
+// v_mfma_i32_16x16x64_i8 wants 16 bytes of row lane % 16 in a lane.  Loaded like that, straight into registers, neighbouring lanes
+// lie in different rows and the memory pipe takes one lane a cycle: 64 cycles per KiB, which bounded 4096 x 14336 at 16 tokens by the loads of both
+// operands (14.6 us, 10.6 with one token, whose codes all lanes share; a plain read of the weights 10.1).  So both go into LDS by loads that
+// write there, 128 neighbouring bytes of a row at a time, RING steps at once, and come back as operands; the eight 16-byte
+// parts of a row sit XOR-permuted by half the row's number, so that sixteen rows' reads use all banks.
 //
 // Bound by the weights' bytes.
+#include <type_traits>
+
 #include "bcq_int8.hpp"
+#include "bcq_internal.hpp"
 
 namespace bcq {
 namespace {
@@ -21,90 +27,142 @@ struct RowsParams {
     bool bf16;
 };
 
-// TT: tiles of 16 tokens; MATS: matrices; BLOCKS: blocks of 16 rows of each; WAVES per workgroup
-template <int TT, int MATS, int BLOCKS, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void int8_rows_kernel(const RowsParams a)
-{
-    constexpr int FRAGS = MATS * BLOCKS * TT;
-    constexpr int UNROLL = TT + MATS * BLOCKS <= 2 ? 8 : TT + MATS * BLOCKS <= 4 ? 4 : 2;     // steps whose operands are under way together
-    __shared__ v4i parts[WAVES][FRAGS][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r16 = lane & 15, part = lane >> 4;
-    const int64_t row0 = (int64_t)blockIdx.x * (16 * BLOCKS);
+constexpr int kStep = 128;
 
-    // rows and tokens past the end repeat the last one (their results are not stored)
-    const int8_t *w_at[MATS * BLOCKS], *q_at[TT];
+// TT: tiles of 16 tokens, or 0 for one of eight; MATS: matrices; BLOCKS: blocks of 16 rows of each; WAVES per workgroup; RING steps in LDS
+template <int TT_, int MATS_, int BLOCKS_, int WAVES_, int RING_>
+struct RowsShape {
+    static constexpr int TT = TT_ ? TT_ : 1, MATS = MATS_, BLOCKS = BLOCKS_, WAVES = WAVES_, RING = RING_;
+    static constexpr int WF = MATS * BLOCKS, FRAGS = WF * TT;
+    static constexpr int Q_LOADS = TT_ ? 2 * TT_ : 1, LOADS = 2 * WF + Q_LOADS;    // of 1 KiB: eight rows of 128 bytes
+    static constexpr int TOKEN_ROWS = 8 * Q_LOADS;
+    static constexpr int STAGE = LOADS * 1024;
+    static constexpr int PARTS = WAVES * FRAGS * 1024;                  // the waves' sums
+    static constexpr int BYTES = WAVES * RING * STAGE > PARTS ? WAVES * RING * STAGE : PARTS;
+};
+
+template <typename S>
+__global__ __launch_bounds__(S::WAVES * 64) void int8_rows_kernel(const RowsParams a)
+{
+    constexpr int TT = S::TT, MATS = S::MATS, BLOCKS = S::BLOCKS, WAVES = S::WAVES, RING = S::RING, WF = S::WF, FRAGS = S::FRAGS;
+    constexpr int RESULTS = BLOCKS * TT * 256, EACH = (RESULTS + WAVES * 64 - 1) / (WAVES * 64);
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t row0 = (int64_t)blockIdx.x * (16 * BLOCKS);
+    const uint32_t rows = (uint32_t)min((int64_t)(16 * BLOCKS), a.m - row0), n = (uint32_t)a.n;
+
+    // Load k of a matrix brings rows 8k .. 8k+7; lane l delivers the part that belongs at place l % 8 of row 8k + l / 8.  Rows and tokens past the
+    // end repeat the last one (their results are not stored).
+    uint32_t w_src[2 * BLOCKS], q_src[S::Q_LOADS], part[2];
 #pragma unroll
-    for (int f = 0; f < MATS * BLOCKS; ++f) {
-        const int64_t row = min(row0 + (f % BLOCKS) * 16 + r16, a.m - 1);
-        w_at[f] = a.w[f / BLOCKS] + row * a.n + part * 16;
-    }
+    for (int k = 0; k < 2; ++k) part[k] = ((lane & 7) ^ (((8 * k + (lane >> 3)) >> 1) & 7)) * 16;
 #pragma unroll
-    for (int t = 0; t < TT; ++t) q_at[t] = a.q + (int64_t)min(t * 16 + r16, a.tokens - 1) * a.n + part * 16;
+    for (int k = 0; k < 2 * BLOCKS; ++k) w_src[k] = min((uint32_t)(8 * k + (lane >> 3)), rows - 1) * n;
+#pragma unroll
+    for (int k = 0; k < S::Q_LOADS; ++k) q_src[k] = min((uint32_t)(8 * k + (lane >> 3)), (uint32_t)a.tokens - 1) * n;
+
+    const int stages = (int)((n + kStep - 1) / kStep);
+    const int each = (stages + WAVES - 1) / WAVES;
+    const int first = min(wave * each, stages), end = min(first + each, stages);
+    unsigned char *const mine = lds + wave * RING * S::STAGE;
+    // Columns of step s into a buffer; in a last step parts past the row's end bring the row's first part instead: what is multiplied with them is
+    // set to zero.
+    auto stage = [&](int buffer, int s) {
+        unsigned char *to = mine + buffer * S::STAGE;
+        const uint32_t k0 = (uint32_t)s * kStep;
+        uint32_t column[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) column[k] = k0 + part[k] >= n ? 0u : k0 + part[k];
+#pragma unroll
+        for (int f = 0; f < MATS; ++f) {
+            const auto w_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(a.w[f] + row0 * n), 0, (int)(rows * n), 0x00020000);
+#pragma unroll
+            for (int k = 0; k < 2 * BLOCKS; ++k)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(w_rsrc, (__attribute__((address_space(3))) void *)(to + (f * 2 * BLOCKS + k) * 1024), 16,
+                                                         (int)(w_src[k] + column[k & 1]), 0, 0, 0);
+        }
+        const auto q_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(a.q), 0, (int)((uint32_t)a.tokens * n), 0x00020000);
+#pragma unroll
+        for (int k = 0; k < S::Q_LOADS; ++k)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(q_rsrc, (__attribute__((address_space(3))) void *)(to + (2 * WF + k) * 1024), 16,
+                                                     (int)(q_src[k] + column[k & 1]), 0, 0, 0);
+    };
 
     v4i acc[FRAGS];
 #pragma unroll
     for (int f = 0; f < FRAGS; ++f) acc[f] = v4i{0, 0, 0, 0};
-
-    const int steps = a.n >> 6;                         // whole steps of 64 columns
-    const int each = (steps + WAVES - 1) / WAVES;
-    const int first = min(wave * each, steps), end = min(first + each, steps);
-    auto products = [&](const v4i *w, const v4i *x) {
+    const uint32_t r16 = lane & 15, quarter = lane >> 4;
+    const uint32_t w_row = r16 * kStep, q_row = min(r16, (uint32_t)S::TOKEN_ROWS - 1) * kStep;
+    const uint32_t w_swz = (r16 >> 1) & 7, q_swz = (min(r16, (uint32_t)S::TOKEN_ROWS - 1) >> 1) & 7;
+    auto multiply = [&](int buffer, auto whole, int s) {
+        const unsigned char *from = mine + buffer * S::STAGE;
 #pragma unroll
-        for (int f = 0; f < MATS * BLOCKS; ++f)
+        for (int kk = 0; kk < 2; ++kk) {
+            const uint32_t p = 4 * kk + quarter;
+            v4i w[WF], x[TT];
 #pragma unroll
-            for (int t = 0; t < TT; ++t) acc[f * TT + t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[f], x[t], acc[f * TT + t], 0, 0, 0);
-    };
-    int s = first;
-    for (; s + UNROLL <= end; s += UNROLL) {
-        v4i w[UNROLL][MATS * BLOCKS], x[UNROLL][TT];
+            for (int f = 0; f < WF; ++f) w[f] = *reinterpret_cast<const v4i *>(from + f * 2048 + w_row + ((p ^ w_swz) << 4));
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
+            for (int t = 0; t < TT; ++t) {
+                x[t] = *reinterpret_cast<const v4i *>(from + WF * 2048 + t * 2048 + q_row + ((p ^ q_swz) << 4));
+                if (!decltype(whole)::value && (uint32_t)s * kStep + p * 16 >= n) x[t] = v4i{0, 0, 0, 0};
+            }
 #pragma unroll
-            for (int f = 0; f < MATS * BLOCKS; ++f) w[u][f] = *reinterpret_cast<const v4i *>(w_at[f] + (s + u) * 64);
+            for (int f = 0; f < WF; ++f)
 #pragma unroll
-            for (int t = 0; t < TT; ++t) x[u][t] = *reinterpret_cast<const v4i *>(q_at[t] + (s + u) * 64);
+                for (int t = 0; t < TT; ++t) acc[f * TT + t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[f], x[t], acc[f * TT + t], 0, 0, 0);
         }
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) products(w[u], x[u]);
+    };
+
+    constexpr int AHEAD = RING - 1, UNDER_WAY = (AHEAD - 1) * S::LOADS;
+    for (int b = 0; b < min(AHEAD, end - first); ++b) stage(b, first + b);
+    int buffer = 0, into = AHEAD, s = first;
+    auto next = [](int b) { return b + 1 == RING ? 0 : b + 1; };
+    // (a step that may be the last and end in the middle is never among these: there is at least one behind it)
+    for (; s + AHEAD < end; ++s) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(UNDER_WAY) : "memory");
+        stage(into, s + AHEAD);
+        multiply(buffer, std::true_type{}, s);
+        buffer = next(buffer);
+        into = next(into);
     }
+    // the scales of this thread's results, beside the last operands: neighbouring threads take neighbouring rows
+    float ts[EACH], cs[EACH][MATS];
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        const int e = k * WAVES * 64 + threadIdx.x;
+        ts[k] = a.token_scales[min(e / (16 * BLOCKS), a.tokens - 1)];
+#pragma unroll
+        for (int i = 0; i < MATS; ++i) cs[k][i] = a.channel_scales[i][min(row0 + e % (16 * BLOCKS), a.m - 1)];
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     for (; s < end; ++s) {
-        v4i w[MATS * BLOCKS], x[TT];
-#pragma unroll
-        for (int f = 0; f < MATS * BLOCKS; ++f) w[f] = *reinterpret_cast<const v4i *>(w_at[f] + s * 64);
-#pragma unroll
-        for (int t = 0; t < TT; ++t) x[t] = *reinterpret_cast<const v4i *>(q_at[t] + s * 64);
-        products(w, x);
-    }
-    const int rest = a.n & 63;                          // 0, 16, 32 or 48 columns more: the last wave's, parts past the end are zeros
-    if (rest && wave == WAVES - 1) {
-        const bool there = part * 16 < rest;
-        v4i w[MATS * BLOCKS], x[TT];
-#pragma unroll
-        for (int f = 0; f < MATS * BLOCKS; ++f) w[f] = there ? *reinterpret_cast<const v4i *>(w_at[f] + steps * 64) : v4i{0, 0, 0, 0};
-#pragma unroll
-        for (int t = 0; t < TT; ++t) x[t] = there ? *reinterpret_cast<const v4i *>(q_at[t] + steps * 64) : v4i{0, 0, 0, 0};
-        products(w, x);
+        multiply(buffer, std::false_type{}, s);
+        buffer = next(buffer);
     }
 
+    __syncthreads();                                    // (the rings are read out: their place is the sums')
+    v4i *const parts = reinterpret_cast<v4i *>(lds);
 #pragma unroll
-    for (int f = 0; f < FRAGS; ++f) parts[wave][f][lane] = acc[f];
+    for (int f = 0; f < FRAGS; ++f) parts[(wave * FRAGS + f) * 64 + lane] = acc[f];
     __syncthreads();
-    // element i of lane l: row 4 (l / 16) + i of its block, token l % 16 of its tile; here neighbouring threads take neighbouring rows
-    const int *sums = reinterpret_cast<const int *>(parts);
-    for (int e = threadIdx.x; e < BLOCKS * TT * 256; e += WAVES * 64) {
+    // element i of lane l: row 4 (l / 16) + i of its block, token l % 16 of its tile
+    const int *sums = reinterpret_cast<const int *>(lds);
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        const int e = k * WAVES * 64 + threadIdx.x;
         const int r = e % (16 * BLOCKS), tok = e / (16 * BLOCKS);
         const int64_t row = row0 + r;
         if (row >= a.m || tok >= a.tokens) continue;
         float v[MATS];
 #pragma unroll
-        for (int k = 0; k < MATS; ++k) {
-            const int frag = (k * BLOCKS + r / 16) * TT + tok / 16;
+        for (int i = 0; i < MATS; ++i) {
+            const int frag = (i * BLOCKS + r / 16) * TT + tok / 16;
             const int at = (frag * 64 + (tok % 16) + 16 * ((r % 16) >> 2)) * 4 + (r & 3);
             int sum = 0;
 #pragma unroll
             for (int p = 0; p < WAVES; ++p) sum += sums[p * FRAGS * 256 + at];
-            v[k] = (float)sum * a.token_scales[tok] * a.channel_scales[k][row];
+            v[i] = (float)sum * ts[k] * cs[k][i];
         }
         float out = v[0], slope;
         if constexpr (MATS == 2) out = activate<false>(v[0], a.activation, slope) * v[MATS - 1];
@@ -112,23 +170,44 @@ __global__ __launch_bounds__(WAVES * 64) void int8_rows_kernel(const RowsParams 
     }
 }
 
-template <int TT, int MATS, int BLOCKS, int WAVES>
+template <int TT, int MATS, int BLOCKS, int WAVES, int RING>
 hipError_t go(const RowsParams &p, hipStream_t stream)
 {
+    using S = RowsShape<TT, MATS, BLOCKS, WAVES, RING>;
+    static_assert(S::BYTES <= 160 * 1024, "LDS of a CU");
     const int64_t blocks = (p.m + 16 * BLOCKS - 1) / (16 * BLOCKS);
-    hipLaunchKernelGGL((int8_rows_kernel<TT, MATS, BLOCKS, WAVES>), dim3((unsigned)blocks), dim3(WAVES * 64), 0, stream, p);
+    const auto kernel = int8_rows_kernel<S>;
+    if (hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), S::BYTES)) return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(WAVES * 64), S::BYTES, stream, p);
     return hipGetLastError();
+}
+
+template <int MATS>
+hipError_t pick(const RowsParams &p, hipStream_t stream)
+{
+    const bool tall = p.m * MATS >= 8192;
+    if (p.tokens <= 8) return go<0, MATS, 1, 4, 3>(p, stream);
+    if (p.tokens <= 16) return go<1, MATS, 1, 4, 3>(p, stream);
+    // More tokens' codes are worth two blocks of rows, where those still give every CU a workgroup: 14336 x 4096 with 32 tokens 13.6 -> 11.3 us,
+    // with 64 tokens 21.4 -> 16.2; 4096 x 14336 the other way, 11.4 and 16.1 against 15.7 and 18.5.
+    if (p.tokens <= 32) return tall ? go<2, MATS, 2, 4, 2>(p, stream) : go<2, MATS, 1, 4, 3>(p, stream);
+    if constexpr (MATS == 1)
+        if (tall) return go<4, 1, 2, 4, 3>(p, stream);
+    return go<4, MATS, 1, 4, 3>(p, stream);
 }
 
 }  // namespace
 
-bool int8_rows_supports(const Int8Args &a) { return a.tokens <= 16; }
+// Up to 32 tokens, and up to 64 on matrices of at most 12288 rows (gate and up together): beyond that a workgroup moves more bytes of tokens' codes
+// than of weights, and the tiles of 64 x 64 are ahead (14336 x 4096 with 48 tokens 14.8 against 14.4 us, gated 31.1 against 27.6;
+// 4096 x 14336 14.2 against 26.1).
+bool int8_rows_supports(const Int8Args &a) { return a.tokens <= 32 || (a.tokens <= 64 && a.m * a.matrices <= 12288); }
 
 hipError_t int8_rows_launch(const Int8Args &a, hipStream_t stream)
 {
-    RowsParams p{a.q, {a.w[0], a.w[1]}, a.token_scales, {a.channel_scales[0], a.channel_scales[1]}, a.y, a.m, (int)a.n, (int)a.tokens, a.activation, a.bf16};
-    if (a.matrices == 2) return go<1, 2, 1, 8>(p, stream);
-    return go<1, 1, 1, 8>(p, stream);
+    const RowsParams p{a.q, {a.w[0], a.w[1]}, a.token_scales, {a.channel_scales[0], a.channel_scales[1]}, a.y, a.m, (int)a.n, (int)a.tokens,
+                       a.activation, a.bf16};
+    return a.matrices == 2 ? pick<2>(p, stream) : pick<1>(p, stream);
 }
 
 }  // namespace bcq
