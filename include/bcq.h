@@ -269,14 +269,14 @@ int bcq_int8_gated(const int8_t *q, const float *token_scales, const int8_t *w_g
  *     dgate_scales[r] = sum_t dg[t][r] token_scales[t] sum_j q[t][j] w_gate[r][j],   dup_scales likewise with du and w_up
  *   dy, dh      [tokens][m] of `type`
  *   dx          [tokens][n] of `type` (written); gradients of the scales: float [m] (written)
- *   workspace   at least bcq_int8_backward_workspace(matrices, m, tokens) bytes, 256-byte aligned, contents irrelevant before
+ *   workspace   at least bcq_int8_backward_workspace(matrices, m, n, tokens) bytes, 256-byte aligned, contents irrelevant before
  *               and after; matrices: 1 for bcq_int8_gemm_backward, 2 for bcq_int8_gated_backward.  Calls that may run at the same time
  *               need one each.
  * The gradients of the projections are held in 11 bits on their way into the product with the weights, scaled per token so that dy's range does
  * not matter.  Sums have a fixed order: the same call gives the same bits.
  * bcq_int8_backward_workspace returns BCQ_ERR_BAD_SHAPE for sizes that the calls refuse.  Host call.
  */
-int64_t bcq_int8_backward_workspace(int matrices, int64_t m, int64_t tokens);
+int64_t bcq_int8_backward_workspace(int matrices, int64_t m, int64_t n, int64_t tokens);
 int bcq_int8_gemm_backward(const void *dy, const int8_t *q, const float *token_scales, const int8_t *w, const float *channel_scales,
                            void *dx, float *dchannel_scales, int type, int64_t m, int64_t n, int64_t tokens, void *workspace,
                            int64_t workspace_bytes, void *stream);

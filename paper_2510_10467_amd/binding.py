@@ -100,7 +100,7 @@ def lib() -> ctypes.CDLL:
         L.bcq_int8_quantize.argtypes = [vp, i32, vp, vp, i64, i64, vp]
         L.bcq_int8_gemm.argtypes = [vp, vp, vp, vp, vp, i32, i64, i64, i64, vp]
         L.bcq_int8_gated.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, i32, i64, i64, i64, vp]
-        L.bcq_int8_backward_workspace.argtypes = [i32, i64, i64]
+        L.bcq_int8_backward_workspace.argtypes = [i32, i64, i64, i64]
         L.bcq_int8_backward_workspace.restype = i64
         L.bcq_int8_gemm_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i64, i64, i64, vp, i64, vp]
         L.bcq_int8_gated_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, i32, i64, i64, i64, vp, i64, vp]
@@ -438,7 +438,7 @@ def _int8_backward_setup(where: str, dy, tokens: int, m: int, n: int, matrices: 
     if dy.shape != (tokens, m) or dy.device != like.device:
         raise ValueError(f"{where}: the gradient has the wrong shape or device")
     kind = _type(dy.dtype, where)
-    size = lib().bcq_int8_backward_workspace(matrices, m, tokens)
+    size = lib().bcq_int8_backward_workspace(matrices, m, n, tokens)
     _check(min(size, 0), where)
     return (kind, torch.empty((tokens, n), dtype=dy.dtype, device=like.device), size,
             torch.empty((size,), dtype=torch.uint8, device=like.device))

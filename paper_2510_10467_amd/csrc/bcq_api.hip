@@ -200,7 +200,7 @@ int run_int8_backward(bcq::Int8Args a, const void *dy, void *dx, void *workspace
     if (!aligned(dy, 2) || !aligned(a.q, 16) || !aligned(a.token_scales, 4) || !aligned(dx, 16) || !aligned(a.dscales[0], 4) ||
         !aligned(a.dscales[1], 4) || !aligned(workspace, 256))
         return BCQ_ERR_ALIGN;
-    if (workspace_bytes < bcq::int8_workspace(a.matrices, a.m, a.tokens).bytes) return BCQ_ERR_WORKSPACE;
+    if (workspace_bytes < bcq::int8_workspace(a.matrices, a.m, a.n, a.tokens).bytes) return BCQ_ERR_WORKSPACE;
     a.dy = static_cast<const uint16_t *>(dy);
     a.dx = static_cast<uint16_t *>(dx);
     a.workspace = workspace;
@@ -509,11 +509,11 @@ int bcq_int8_gated(const int8_t *q, const float *token_scales, const int8_t *w_g
     return run_int8(int8_args(q, token_scales, w_gate, gate_scales, w_up, up_scales, 2, activation, h, type, m, n, tokens), stream);
 }
 
-int64_t bcq_int8_backward_workspace(int matrices, int64_t m, int64_t tokens)
+int64_t bcq_int8_backward_workspace(int matrices, int64_t m, int64_t n, int64_t tokens)
 {
     if (matrices < 1 || matrices > 2) return BCQ_ERR_BAD_SHAPE;
-    if (int rc = check_int8(BCQ_FLOAT16, BCQ_ACT_SILU, m, 16, tokens, kInt8MaxBackwardRows)) return rc;
-    return bcq::int8_workspace(matrices, m, tokens).bytes;
+    if (int rc = check_int8(BCQ_FLOAT16, BCQ_ACT_SILU, m, n, tokens, kInt8MaxBackwardRows)) return rc;
+    return bcq::int8_workspace(matrices, m, n, tokens).bytes;
 }
 
 int bcq_int8_gemm_backward(const void *dy, const int8_t *q, const float *token_scales, const int8_t *w, const float *channel_scales,

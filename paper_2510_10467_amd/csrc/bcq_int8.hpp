@@ -78,10 +78,11 @@ hipError_t int8_tile_launch(const Int8Args &a, hipStream_t stream);
 // The backward passes' workspace, in this order.
 struct Int8Workspace {
     int64_t grad_stride;            // halves between tokens: matrices * m rounded up to 64
-    int64_t grad, norms, scale_top, parts, bytes;       // offsets in bytes, and the whole
+    int splits;                     // runs of channels whose contributions to dx are summed apart
+    int64_t grad, norms, scale_top, parts, split_sums, bytes;       // offsets in bytes, and the whole
     int64_t part_count;             // room for so many partial sums of a channel
 };
-Int8Workspace int8_workspace(int matrices, int64_t m, int64_t tokens);
+Int8Workspace int8_workspace(int matrices, int64_t m, int64_t n, int64_t tokens);
 // the gradients of the projections, scaled as int8_backward_* explains, and partial sums of the channel scales' gradients
 hipError_t int8_tile_backward_launch(const Int8Args &a, const Int8Workspace &ws, hipStream_t stream, int64_t &part_count);
 hipError_t int8_backward_launch(const Int8Args &a, hipStream_t stream);

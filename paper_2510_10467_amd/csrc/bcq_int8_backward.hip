@@ -20,27 +20,47 @@ typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef int v2i __attribute__((ext_vector_type(2)));
 
-// One workgroup per token, and a last one for the scales.
+// One workgroup per token, and a first one for the scales.  Four loads of a thread are under way at a time.
 __global__ __launch_bounds__(256) void int8_norms_kernel(const uint16_t *__restrict__ dy, const float *__restrict__ c0, const float *__restrict__ c1,
-                                                         float *__restrict__ norms, float *__restrict__ scale_top, int64_t m, int64_t tokens, bool bf16,
-                                                         bool whole)
+                                                         float *__restrict__ norms, float *__restrict__ scale_top, int64_t m, bool bf16, bool whole)
 {
     __shared__ float tops[4];
     float top = 0.f;                                    // (a NaN leaves it as it is: such a token's results are NaN whatever its power)
-    const int64_t token = blockIdx.x;
-    if (token < tokens) {
-        const uint16_t *row = dy + token * m;
-        if (whole) {
-            for (int64_t j = threadIdx.x; j * 8 < m; j += 256) {
-                const u32x4 v = *reinterpret_cast<const u32x4 *>(row + j * 8);
+    const bool for_scales = blockIdx.x == 0;
+    const int64_t token = (int64_t)blockIdx.x - 1;
+    const int last = (int)m - 1;                        // what lies past the end counts the last value again
+    if (for_scales) {
+        for (int j = threadIdx.x; j <= last; j += 2048) {
+            float v[8], u[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(from_16(v[i] & 0xffffu, bf16)), fabsf(from_16(v[i] >> 16, bf16))));
+            for (int k = 0; k < 8; ++k) {
+                v[k] = c0[min(j + k * 256, last)];
+                u[k] = c1[min(j + k * 256, last)];
             }
-        } else {
-            for (int64_t j = threadIdx.x; j < m; j += 256) top = fmaxf(top, fabsf(from_16(row[j], bf16)));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) top = fmaxf(top, fmaxf(fabsf(v[k]), fabsf(u[k])));
+        }
+    } else if (whole) {
+        const u32x4 *row = reinterpret_cast<const u32x4 *>(dy + token * m);
+        const int last_piece = (int)(m / 8) - 1;
+        for (int j = threadIdx.x; j <= last_piece; j += 1024) {
+            u32x4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = row[min(j + k * 256, last_piece)];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(from_16(v[k][i] & 0xffffu, bf16)), fabsf(from_16(v[k][i] >> 16, bf16))));
         }
     } else {
-        for (int64_t j = threadIdx.x; j < m; j += 256) top = fmaxf(top, fmaxf(fabsf(c0[j]), fabsf(c1[j])));
+        const uint16_t *row = dy + token * m;
+        for (int j = threadIdx.x; j <= last; j += 1024) {
+            uint32_t v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = row[min(j + k * 256, last)];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) top = fmaxf(top, fabsf(from_16(v[k], bf16)));
+        }
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
@@ -50,17 +70,26 @@ __global__ __launch_bounds__(256) void int8_norms_kernel(const uint16_t *__restr
     top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
     const bool usable = top > 0.f && top < __builtin_inff();
     const int e = usable ? min(max(ilogbf(top), -120), 120) : 0;
-    if (token < tokens) norms[token] = ldexpf(1.f, usable ? -5 - e : 0);
-    else *scale_top = ldexpf(1.f, usable ? e + 1 : 0);
+    if (for_scales) *scale_top = ldexpf(1.f, usable ? e + 1 : 0);
+    else norms[token] = ldexpf(1.f, usable ? -5 - e : 0);
 }
 
-__global__ __launch_bounds__(256) void int8_sums_kernel(const float *__restrict__ parts, float *__restrict__ d0, float *__restrict__ d1, int64_t m,
-                                                        int matrices, int64_t part_count)
+// In the partial sums' order; eight are under way at a time.
+__global__ __launch_bounds__(64) void int8_sums_kernel(const float *__restrict__ parts, float *__restrict__ d0, float *__restrict__ d1, int64_t m,
+                                                       int matrices, int64_t part_count)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= m * matrices) return;
+    const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x, stride = m * matrices;
+    if (i >= stride) return;
     float sum = 0.f;
-    for (int64_t p = 0; p < part_count; ++p) sum += parts[p * m * matrices + i];
+    int64_t p = 0;
+    for (; p + 8 <= part_count; p += 8) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = parts[(p + k) * stride + i];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += v[k];
+    }
+    for (; p < part_count; ++p) sum += parts[p * stride + i];
     if (i < m) d0[i] = sum;
     else d1[i - m] = sum;
 }
@@ -73,16 +102,24 @@ struct SecondParams {
     uint32_t m, m_padded, n, tokens, grad_stride;
     uint32_t column_tiles, token_tiles;
     int matrices;
-    bool bf16, whole;
+    bool bf16;
+    // the steps in `splits` runs, each its own grid row, whose sums go to split_sums [splits][tokens][n] (one run: straight to dx)
+    int splits;
+    float *split_sums;
 };
 
-template <int WC_, int WT_, int FC_, int FT_>
+// FC x FT tiles of 32 columns x 32 tokens in a wave, WC x WT waves in a team, RING buffers of each team, STEP rows of the weights at a time
+template <int WC_, int WT_, int FC_, int FT_, int RING_, int TEAMS_ = 1, int STEP_ = 64, bool ACROSS_ = (RING_ >= 4)>
 struct SecondShape {
-    static constexpr int WC = WC_, WT = WT_, FC = FC_, FT = FT_;
-    static constexpr int COLS = WC * FC * 32, TOKS = WT * FT * 32, WAVES = WC * WT;
-    static constexpr int W_BYTES = 64 * COLS, STAGE = W_BYTES + TOKS * 128;
+    static constexpr int WC = WC_, WT = WT_, FC = FC_, FT = FT_, RING = RING_, TEAMS = TEAMS_, STEP = STEP_;
+    static constexpr bool ACROSS = ACROSS_;
+    static constexpr int COLS = WC * FC * 32, TOKS = WT * FT * 32, TEAM_WAVES = WC * WT, WAVES = TEAMS * TEAM_WAVES;
+    static constexpr int G_ROW = STEP * 2, W_BYTES = STEP * COLS, STAGE = W_BYTES + TOKS * G_ROW;
+    static constexpr int PLACES = G_ROW / 16, LOAD_TOKS = 64 / PLACES;          // 16-byte parts of a token's row in LDS, tokens of a load
+    static constexpr __device__ __host__ uint32_t swizzle(uint32_t tok) { return tok * PLACES / 16 % PLACES; }
     static constexpr int OUT_ROW = COLS * 2 + 16, OUT = TOKS * OUT_ROW;
-    static constexpr int BYTES = 2 * STAGE > OUT ? 2 * STAGE : OUT;
+    static constexpr int RINGS = TEAMS * RING * STAGE, EXCHANGE = (TEAMS - 1) * COLS * TOKS * 4;
+    static constexpr int BYTES = RINGS > OUT ? (RINGS > EXCHANGE ? RINGS : EXCHANGE) : (OUT > EXCHANGE ? OUT : EXCHANGE);
 };
 
 // Eight codes to binary16: 1024 + (code + 128), less 1152.
@@ -99,14 +136,15 @@ __device__ __forceinline__ v8h halves_of(v2i codes)
     return __builtin_bit_cast(v8h, out);
 }
 
-// A step is 64 rows of the weights: an LDS row holds COLS codes, its 16-byte parts XOR-permuted by the row's number; a token's 64
-// gradients are a row of 128 bytes, permuted as in the first half.
+// A step is STEP rows of the weights: an LDS row holds COLS codes, its 16-byte parts XOR-permuted by the row's number; a token's STEP
+// gradients are a row too, permuted as in the first half.
 template <typename S>
-__global__ __launch_bounds__(S::WAVES * 64) void int8_second_kernel(const SecondParams a)
+__global__ __launch_bounds__(S::WAVES * 64, 2) void int8_second_kernel(const SecondParams a)
 {
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wc = wave / S::WT, wt = wave % S::WT;
+    const int team = wave / S::TEAM_WAVES, tw = wave % S::TEAM_WAVES;
+    const int wc = tw / S::WT, wt = tw % S::WT;
     const int r32 = lane & 31, half = lane >> 5;
 
     const uint32_t total = gridDim.x, xcd = blockIdx.x & 7;
@@ -117,41 +155,44 @@ __global__ __launch_bounds__(S::WAVES * 64) void int8_second_kernel(const Second
     const uint32_t c0 = rest / in_group * S::COLS, t0 = (group * 8 + rest % in_group) * S::TOKS;
     const uint32_t cols = min((uint32_t)S::COLS, a.n - c0), toks = min((uint32_t)S::TOKS, a.tokens - t0);
 
-    constexpr int W_LOADS = S::W_BYTES / 1024 / S::WAVES, G_LOADS = S::TOKS / 8 / S::WAVES;
+    constexpr int W_LOADS = S::W_BYTES / 1024 / S::TEAM_WAVES, G_LOADS = S::TOKS / S::LOAD_TOKS / S::TEAM_WAVES;
     constexpr int PARTS = S::COLS / 16, ROWS_PER = 64 / PARTS;          // parts of an LDS row, rows of a load
-    static_assert(W_LOADS * 1024 * S::WAVES == S::W_BYTES && G_LOADS * 8 * S::WAVES == S::TOKS, "whole loads per wave");
+    static_assert(W_LOADS * 1024 * S::TEAM_WAVES == S::W_BYTES && G_LOADS * S::LOAD_TOKS * S::TEAM_WAVES == S::TOKS, "whole loads per wave");
     uint32_t g_src[G_LOADS];
 #pragma unroll
     for (int k = 0; k < G_LOADS; ++k) {
-        const uint32_t tok = 8 * (wave * G_LOADS + k) + (lane >> 3);
-        g_src[k] = min(tok, toks - 1) * a.grad_stride * 2 + ((lane & 7) ^ ((tok >> 1) & 7)) * 16;
+        const uint32_t tok = S::LOAD_TOKS * (tw * G_LOADS + k) + lane / S::PLACES;
+        g_src[k] = min(tok, toks - 1) * a.grad_stride * 2 + (lane % S::PLACES ^ S::swizzle(tok)) * 16;
     }
     // load k of the weights: rows ROWS_PER * unit .. of the step, place lane % PARTS (columns past the end bring the last part)
     uint32_t w_row[W_LOADS], w_col[W_LOADS];
 #pragma unroll
     for (int k = 0; k < W_LOADS; ++k) {
-        w_row[k] = (wave * W_LOADS + k) * ROWS_PER + lane / PARTS;
+        w_row[k] = (tw * W_LOADS + k) * ROWS_PER + lane / PARTS;
         w_col[k] = min((uint32_t)((lane % PARTS) ^ (w_row[k] & (PARTS - 1))) * 16, cols - 16);
     }
-    const auto g_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16 *>(a.grad + (int64_t)t0 * a.grad_stride), 0,
-                                                          (int)(toks * a.grad_stride * 2), 0x00020000);
-    const uint32_t per_matrix = a.m_padded / 64;
-    const int steps = (int)(per_matrix * a.matrices);
+    const _Float16 *const g_base = a.grad + (int64_t)t0 * a.grad_stride;
+    const uint32_t per_matrix = a.m_padded / S::STEP;
+    const int all_steps = (int)(per_matrix * a.matrices), run = (all_steps + a.splits - 1) / a.splits;
+    const int first_step = (int)blockIdx.y * run, steps = max(0, min(run, all_steps - first_step));
+    unsigned char *const mine = lds + team * S::RING * S::STAGE;        // the team's ring
     // Rows past a matrix's end repeat its last one: the gradients there are zeros.
-    auto stage = [&](int buffer, uint32_t s) {
-        unsigned char *to = lds + buffer * S::STAGE;
-        const uint32_t k = s >= per_matrix ? 1 : 0, row0 = (s - k * per_matrix) * 64;
-        const uint32_t rows = min(64u, a.m - row0);
+    auto stage = [&](int buffer, uint32_t of_run) {
+        unsigned char *to = mine + buffer * S::STAGE;
+        const uint32_t s = first_step + of_run;
+        const uint32_t k = s >= per_matrix ? 1 : 0, row0 = min((s - k * per_matrix) * S::STEP, a.m - 1);
+        const uint32_t rows = min((uint32_t)S::STEP, a.m - row0);
         const auto w_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>((k ? a.w[1] : a.w[0]) + (int64_t)row0 * a.n + c0), 0,
                                                               (int)((rows - 1) * a.n + cols), 0x00020000);
+        const auto g_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16 *>(g_base), 0, (int)(toks * a.grad_stride * 2), 0x00020000);
 #pragma unroll
         for (int j = 0; j < W_LOADS; ++j)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(w_rsrc, (__attribute__((address_space(3))) void *)(to + (wave * W_LOADS + j) * 1024), 16,
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(w_rsrc, (__attribute__((address_space(3))) void *)(to + (tw * W_LOADS + j) * 1024), 16,
                                                      (int)(min(w_row[j], rows - 1) * a.n + w_col[j]), 0, 0, 0);
 #pragma unroll
         for (int j = 0; j < G_LOADS; ++j)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(g_rsrc, (__attribute__((address_space(3))) void *)(to + S::W_BYTES + (wave * G_LOADS + j) * 1024), 16,
-                                                     (int)g_src[j], (int)(s * 128), 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(g_rsrc, (__attribute__((address_space(3))) void *)(to + S::W_BYTES + (tw * G_LOADS + j) * 1024), 16,
+                                                     (int)g_src[j], (int)(s * S::G_ROW), 0, 0);
     };
 
     v16f acc[S::FC][S::FT];
@@ -162,41 +203,135 @@ __global__ __launch_bounds__(S::WAVES * 64) void int8_second_kernel(const Second
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[c][t][i] = 0.f;
 
-    const uint32_t swz = (r32 >> 1) & 7;
+    const uint32_t swz = S::swizzle(r32);
     // the transposing read: lanes 2 r and 2 r + 1 of sixteen point at the halves of row r's 16 columns; lanes 0-31 take rows 0-7 of a
     // step of 16, lanes 32-63 rows 8-15, of which every second sixteen the next 16 columns
     const int tr_row = half * 8 + ((lane & 15) >> 1);
-    auto multiply = [&](int buffer, int kk) {
-        const unsigned char *from = lds + buffer * S::STAGE;
+    struct Operands {
         v8h w[S::FC], g[S::FT];
+    };
+    auto operands = [&](int buffer, int kk) {
+        const unsigned char *from = mine + buffer * S::STAGE;
+        v2i raw[S::FC];
+        Operands o;
 #pragma unroll
         for (int c = 0; c < S::FC; ++c) {
             const int row = kk * 16 + tr_row;
             const int part = (wc * S::FC + c) * 2 + ((lane >> 4) & 1);
             const unsigned char *at = from + row * S::COLS + ((part ^ (row & (PARTS - 1))) << 4) + (lane & 1) * 8;
-            w[c] = halves_of(__builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i *)at));
+            raw[c] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i *)at);
         }
 #pragma unroll
         for (int t = 0; t < S::FT; ++t)
-            g[t] = *reinterpret_cast<const v8h *>(from + S::W_BYTES + ((wt * S::FT + t) * 32 + r32) * 128 + (((2 * kk + half) ^ swz) << 4));
+            o.g[t] = *reinterpret_cast<const v8h *>(from + S::W_BYTES + ((wt * S::FT + t) * 32 + r32) * S::G_ROW + (((2 * kk + half) ^ swz) << 4));
+#pragma unroll
+        for (int c = 0; c < S::FC; ++c) o.w[c] = halves_of(raw[c]);
+        return o;
+    };
+    auto multiply = [&](const Operands &o) {
 #pragma unroll
         for (int c = 0; c < S::FC; ++c)
 #pragma unroll
-            for (int t = 0; t < S::FT; ++t) acc[c][t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w[c], g[t], acc[c][t], 0, 0, 0);
+            for (int t = 0; t < S::FT; ++t) acc[c][t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.w[c], o.g[t], acc[c][t], 0, 0, 0);
+    };
+    // (as in the first half; between the matrix instructions first the reads, then the codes' conversion)
+    [[maybe_unused]] Operands now;
+    auto whole_step = [&](int buffer, int after) {
+#pragma unroll
+        for (int kk = 0; kk < S::STEP / 16; ++kk) {
+            if constexpr (S::ACROSS) {
+                const Operands later = kk + 1 < S::STEP / 16 ? operands(buffer, kk + 1) : operands(after, 0);
+                multiply(now);
+                now = later;
+                constexpr int PRODUCTS = S::FC * S::FT, BETWEEN = PRODUCTS > 1 ? (10 * S::FC + PRODUCTS - 2) / (PRODUCTS - 1) : 1;
+                __builtin_amdgcn_sched_group_barrier(0x100, S::FC, 0);
+#pragma unroll
+                for (int i = 0; i < PRODUCTS; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    if (i < S::FT) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    if (i > 0) __builtin_amdgcn_sched_group_barrier(0x002, BETWEEN, 0);
+                }
+            } else {
+                multiply(operands(buffer, kk));
+            }
+        }
     };
 
-    stage(0, 0);
-    for (int s = 0; s < steps; ++s) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (s + 1 < steps) stage((s + 1) & 1, (uint32_t)(s + 1));
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) multiply(s & 1, kk);
+    constexpr int AHEAD = S::RING - 1, LOADS = W_LOADS + G_LOADS;
+    static_assert(S::RING >= 3 || !S::ACROSS, "a step reads the next one's first operands");
+    const int rounds = (steps + S::TEAMS - 1) / S::TEAMS;
+    auto step = [&](int i) { return i * S::TEAMS + team; };
+    for (int i = 0; i < min(AHEAD, rounds); ++i)
+        if (step(i) < steps) stage(i, (uint32_t)step(i));
+    if (rounds > AHEAD) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((AHEAD - 1) * LOADS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    if (S::ACROSS) now = operands(0, 0);
+    int buffer = 0, into = AHEAD, i = 0;
+    auto next = [](int b) { return b + 1 == S::RING ? 0 : b + 1; };
+    for (; i + AHEAD < rounds; ++i) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD - (S::ACROSS ? 2 : 1)) * LOADS) : "memory");
+        if (S::TEAMS == 1 || step(i + AHEAD) < steps) stage(into, (uint32_t)step(i + AHEAD));
+        whole_step(buffer, next(buffer));
+        buffer = next(buffer);
+        into = next(into);
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    for (; step(i) < steps; ++i) {
+        whole_step(buffer, next(buffer));
+        buffer = next(buffer);
     }
     __syncthreads();
+    if constexpr (S::TEAMS > 1) {
+        v4f *const exchange = reinterpret_cast<v4f *>(lds) + tw * (S::FC * S::FT * 4 * 64) + lane;
+        constexpr int BETWEEN = S::TEAM_WAVES * S::FC * S::FT * 4 * 64;
+        if (team > 0) {
+#pragma unroll
+            for (int c = 0; c < S::FC; ++c)
+#pragma unroll
+                for (int t = 0; t < S::FT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        exchange[(team - 1) * BETWEEN + ((c * S::FT + t) * 4 + e) * 64] =
+                            v4f{acc[c][t][4 * e], acc[c][t][4 * e + 1], acc[c][t][4 * e + 2], acc[c][t][4 * e + 3]};
+        }
+        __syncthreads();
+        if (team == 0) {
+#pragma unroll
+            for (int k = 0; k < S::TEAMS - 1; ++k)
+#pragma unroll
+                for (int c = 0; c < S::FC; ++c)
+#pragma unroll
+                    for (int t = 0; t < S::FT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const v4f v = exchange[k * BETWEEN + ((c * S::FT + t) * 4 + e) * 64];
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) acc[c][t][4 * e + x] += v[x];
+                        }
+        }
+        __syncthreads();
+    }
 
+    if (a.splits > 1) {
+        if (team > 0) return;
+#pragma unroll
+        for (int t = 0; t < S::FT; ++t) {
+            const uint32_t tok = (wt * S::FT + t) * 32 + r32;
+#pragma unroll
+            for (int c = 0; c < S::FC; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t col = (wc * S::FC + c) * 32 + 8 * e + 4 * half;
+                    if (tok < toks && col < cols)           // (columns come in sixteens)
+                        *reinterpret_cast<v4f *>(a.split_sums + ((int64_t)blockIdx.y * a.tokens + t0 + tok) * a.n + c0 + col) =
+                            v4f{acc[c][t][4 * e], acc[c][t][4 * e + 1], acc[c][t][4 * e + 2], acc[c][t][4 * e + 3]};
+                }
+        }
+        return;
+    }
     const float top = *a.scale_top;
 #pragma unroll
-    for (int t = 0; t < S::FT; ++t) {
+    for (int t = 0; t < (team == 0 ? S::FT : 0); ++t) {
         const uint32_t tok = (wt * S::FT + t) * 32 + r32;
         const float back = 1.f / a.norms[t0 + min(tok, toks - 1)];      // (a power of two)
 #pragma unroll
@@ -219,6 +354,22 @@ __global__ __launch_bounds__(S::WAVES * 64) void int8_second_kernel(const Second
     }
 }
 
+// The runs' sums, in order, to dx: four columns a thread.
+__global__ __launch_bounds__(256) void int8_splits_kernel(const float *__restrict__ split_sums, const float *__restrict__ norms,
+                                                          const float *__restrict__ scale_top, uint16_t *__restrict__ dx, int64_t tokens, uint32_t n,
+                                                          int splits, bool bf16)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, count = tokens * n / 4;
+    if (i >= count) return;
+    v4f sum = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < splits; ++s) sum += reinterpret_cast<const v4f *>(split_sums)[s * count + i];
+    const float top = *scale_top, back = 1.f / norms[i * 4 / n];
+    uint32_t out[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) out[k] = to_16(sum[k] * top * back, bf16);
+    reinterpret_cast<u32x2 *>(dx)[i] = u32x2{out[0] | out[1] << 16, out[2] | out[3] << 16};
+}
+
 template <typename S>
 hipError_t go(SecondParams p, hipStream_t stream)
 {
@@ -226,44 +377,60 @@ hipError_t go(SecondParams p, hipStream_t stream)
     p.token_tiles = (p.tokens + S::TOKS - 1) / S::TOKS;
     const auto kernel = int8_second_kernel<S>;
     if (hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), S::BYTES)) return e;
-    hipLaunchKernelGGL(kernel, dim3(p.column_tiles * p.token_tiles), dim3(S::WAVES * 64), S::BYTES, stream, p);
+    hipLaunchKernelGGL(kernel, dim3(p.column_tiles * p.token_tiles, (unsigned)p.splits), dim3(S::WAVES * 64), S::BYTES, stream, p);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (p.splits == 1) return hipSuccess;
+    const int64_t threads = (int64_t)p.tokens * p.n / 4;
+    hipLaunchKernelGGL(int8_splits_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, p.split_sums, p.norms, p.scale_top, p.dx,
+                       (int64_t)p.tokens, p.n, p.splits, p.bf16);
     return hipGetLastError();
 }
 
-using Large = SecondShape<4, 2, 2, 4>;      // 256 columns x 256 tokens
-using Medium = SecondShape<2, 2, 2, 2>;     // 128 x 128
-using Small = SecondShape<2, 2, 1, 1>;      // 64 x 64
+using Large = SecondShape<2, 2, 2, 4, 2, 2>;            // 128 columns x 256 tokens, two teams
+using Small = SecondShape<2, 2, 1, 1, 4, 2>;            // 64 x 64, two teams
+
+// Few columns and tokens, many channels: the channels in up to eight runs, of 8 steps at least, as long as every CU gets one workgroup (4096 columns,
+// 512 tokens, 2 x 14336 channels: 300 us in one run, 70 in four).
+int second_splits(int matrices, int64_t m, int64_t n, int64_t tokens)
+{
+    const int64_t tiles = ((n + 127) / 128) * ((tokens + 255) / 256), steps = matrices * ((m + 63) / 64);
+    int splits = 1;
+    while (splits < 8 && tiles * splits * 2 <= 256 && steps >= 8 * splits * 2) splits *= 2;
+    return splits;
+}
 
 }  // namespace
 
-Int8Workspace int8_workspace(int matrices, int64_t m, int64_t tokens)
+Int8Workspace int8_workspace(int matrices, int64_t m, int64_t n, int64_t tokens)
 {
     Int8Workspace ws;
     auto up = [](int64_t bytes) { return (bytes + 255) / 256 * 256; };
     ws.grad_stride = matrices * ((m + 63) / 64 * 64);
     ws.part_count = (tokens + 63) / 64 * 2 + 2;             // at most: a wave's tokens are 64, or 32 in tiles of 64
+    ws.splits = second_splits(matrices, m, n, tokens);
     ws.grad = 0;
     ws.norms = up(tokens * ws.grad_stride * 2);
     ws.scale_top = ws.norms + up(tokens * 4);
     ws.parts = ws.scale_top + 256;
-    ws.bytes = ws.parts + up(ws.part_count * matrices * m * 4);
+    ws.split_sums = ws.parts + up(ws.part_count * matrices * m * 4);
+    ws.bytes = ws.split_sums + (ws.splits > 1 ? up(ws.splits * tokens * n * 4) : 0);
     return ws;
 }
 
 hipError_t int8_backward_launch(const Int8Args &a, hipStream_t stream)
 {
-    const Int8Workspace ws = int8_workspace(a.matrices, a.m, a.tokens);
+    const Int8Workspace ws = int8_workspace(a.matrices, a.m, a.n, a.tokens);
     unsigned char *base = static_cast<unsigned char *>(a.workspace);
     float *norms = reinterpret_cast<float *>(base + ws.norms), *scale_top = reinterpret_cast<float *>(base + ws.scale_top);
     int64_t part_count = 0;
     if (a.tokens > 0) {
         const bool whole = a.m % 8 == 0 && (reinterpret_cast<uintptr_t>(a.dy) & 15) == 0;
         hipLaunchKernelGGL(int8_norms_kernel, dim3((unsigned)(a.tokens + 1)), dim3(256), 0, stream, a.dy, a.channel_scales[0],
-                           a.channel_scales[a.matrices - 1], norms, scale_top, a.m, a.tokens, a.bf16, whole);
+                           a.channel_scales[a.matrices - 1], norms, scale_top, a.m, a.bf16, whole);
         if (hipError_t e = hipGetLastError()) return e;
         if (hipError_t e = int8_tile_backward_launch(a, ws, stream, part_count)) return e;
     }
-    hipLaunchKernelGGL(int8_sums_kernel, dim3((unsigned)((a.m * a.matrices + 255) / 256)), dim3(256), 0, stream,
+    hipLaunchKernelGGL(int8_sums_kernel, dim3((unsigned)((a.m * a.matrices + 63) / 64)), dim3(64), 0, stream,
                        reinterpret_cast<const float *>(base + ws.parts), a.dscales[0], a.dscales[a.matrices - 1], a.m, a.matrices, part_count);
     if (hipError_t e = hipGetLastError()) return e;
     if (a.tokens == 0) return hipSuccess;
@@ -281,10 +448,11 @@ hipError_t int8_backward_launch(const Int8Args &a, hipStream_t stream)
     p.grad_stride = (uint32_t)ws.grad_stride;
     p.matrices = a.matrices;
     p.bf16 = a.bf16;
-    auto tiles = [&](int64_t c, int64_t t) { return ((a.n + c - 1) / c) * ((a.tokens + t - 1) / t); };
-    if (tiles(256, 256) >= 256) return go<Large>(p, stream);
-    if (tiles(128, 128) >= 256) return go<Medium>(p, stream);
-    return go<Small>(p, stream);
+    p.splits = ws.splits;
+    p.split_sums = reinterpret_cast<float *>(base + ws.split_sums);
+    // The large tile reads and converts a code for 128 tokens of a wave, the small one for 32, but a handful of tiles leaves most CUs idle.
+    const int64_t large = (int64_t)((p.n + 127) / 128) * ((p.tokens + 255) / 256) * p.splits;
+    return large >= 64 ? go<Large>(p, stream) : go<Small>(p, stream);
 }
 
 }  // namespace bcq

@@ -13,6 +13,8 @@
 //
 // Neighbouring workgroups' numbers go to different XCDs, each with a cache of its own: they are renumbered so that one XCD works on
 // the token tiles of the same weights.
+#include <type_traits>
+
 #include "bcq_int8.hpp"
 #include "bcq_internal.hpp"
 
@@ -35,45 +37,71 @@ struct TileParams {
     float *parts;                   // [token_tiles * WT][matrices][m]
 };
 
-// FR x FT tiles of 32 x 32 in a wave, WR x WT waves
-template <int WR_, int WT_, int FR_, int FT_>
+// FR x FT tiles of 32 x 32 in a wave, WR x WT waves in a team, RING buffers of each team
+template <int WR_, int WT_, int FR_, int FT_, int RING_, int TEAMS_ = 1, int STEP_ = 128, bool ACROSS_ = (RING_ >= 4)>
 struct TileShape {
-    static constexpr int WR = WR_, WT = WT_, FR = FR_, FT = FT_;
-    static constexpr int ROWS = WR * FR * 32, TOKS = WT * FT * 32, WAVES = WR * WT;
+    static constexpr bool ACROSS = ACROSS_;
+    static constexpr int WR = WR_, WT = WT_, FR = FR_, FT = FT_, RING = RING_, TEAMS = TEAMS_;
+    static constexpr int STEP = STEP_;                      // columns of a step, and bytes of an LDS row
+    static constexpr int PLACES = STEP / 16, LOAD_ROWS = 64 / PLACES;          // 16-byte parts of an LDS row, rows of a load
+    // what a part's number is XORed with in a row: sixteen rows' reads of a part use all banks
+    static constexpr __device__ __host__ uint32_t swizzle(uint32_t row) { return row * PLACES / 16 % PLACES; }
+    static constexpr int ROWS = WR * FR * 32, TOKS = WT * FT * 32, TEAM_WAVES = WR * WT, WAVES = TEAMS * TEAM_WAVES;
 };
-
-constexpr int kStep = 128;          // columns, and bytes of an LDS row
 
 template <typename S, int MATS, bool BACKWARD>
 struct TileLds {
-    static constexpr int STAGE = (S::ROWS + S::TOKS) * kStep;
+    static constexpr int STAGE = (S::ROWS + S::TOKS) * S::STEP;
     static constexpr int CHANNELS = S::ROWS / MATS;
     static constexpr int OUT_ROW = CHANNELS * 2 + 16;
     static constexpr int OUT = S::TOKS * OUT_ROW;           // one 16-bit result tile
+    static constexpr int DY_EACH = S::TOKS * CHANNELS / 8 / (S::WAVES * 64);       // pieces of dy's tile for each thread
     static constexpr int OUTS = BACKWARD ? MATS : 1;
     static constexpr int SCALES = OUTS * OUT;               // the channels' scales behind them
     static constexpr int TOKEN_SCALES = SCALES + MATS * CHANNELS * 4;       // the tokens' scales, and their powers of two
     static constexpr int EPILOGUE = TOKEN_SCALES + 2 * S::TOKS * 4;
-    static constexpr int BYTES = 2 * STAGE > EPILOGUE ? 2 * STAGE : EPILOGUE;
+    static constexpr int EXCHANGE = (S::TEAMS - 1) * S::ROWS * S::TOKS * 4;
+    static constexpr int RINGS = S::TEAMS * S::RING * STAGE;
+    static constexpr int BYTES = RINGS > EPILOGUE ? (RINGS > EXCHANGE ? RINGS : EXCHANGE) : (EPILOGUE > EXCHANGE ? EPILOGUE : EXCHANGE);
 };
 
-// Sums over a half wave's 32 lanes of 32 values each: lane l ends with the sum of value l (31 exchanges instead of 160).
+// Sums over a half wave's 32 lanes of 32 values each: lane l ends with the sum of value l.  A step halves the values a lane holds: it keeps those
+// with its own bit of the number and gives the others to a lane whose bit is the other one.  Lanes 16 apart change places in one
+// instruction; the others read across a row of 16 in the addition itself: 8 apart, 7 - l, 2 apart, 1 apart, which together reach all lanes.
+// (Through LDS, 31 exchanges, the sums took 70 of the 380 us of a first half of 2048 tokens and 2 x 14336 channels.)
+template <int CONTROL>
+__device__ __forceinline__ float across(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CONTROL, 0xf, 0xf, true));
+}
+template <int D, int CONTROL>
+__device__ __forceinline__ void halve(float (&v)[32], int lane)
+{
+    const bool upper = lane & D;
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+        const float keep = upper ? v[i + D] : v[i], give = upper ? v[i] : v[i + D];
+        v[i] = keep + across<CONTROL>(give);
+    }
+}
 __device__ __forceinline__ float sums_of_32(float (&v)[32], int lane)
 {
 #pragma unroll
-    for (int d = 16; d >= 1; d /= 2) {
-        const bool upper = lane & d;
-#pragma unroll
-        for (int i = 0; i < d; ++i) {
-            const float keep = upper ? v[i + d] : v[i], give = upper ? v[i] : v[i + d];
-            v[i] = keep + __shfl_xor(give, d, 64);
-        }
+    for (int i = 0; i < 16; ++i) {
+        // rows 1 and 3 of the first change places with rows 0 and 2 of the second
+        const auto swapped = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v[i]), __builtin_bit_cast(uint32_t, v[i + 16]), false, false);
+        const uint32_t own = swapped[0], other = swapped[1];
+        v[i] = __builtin_bit_cast(float, own) + __builtin_bit_cast(float, other);
     }
+    halve<8, 0x128>(v, lane);           // row_ror:8
+    halve<4, 0x141>(v, lane);           // row_half_mirror
+    halve<2, 0x4e>(v, lane);            // quad_perm 2 3 0 1
+    halve<1, 0xb1>(v, lane);            // quad_perm 1 0 3 2
     return v[0];
 }
 
-template <typename S, int MATS, bool BACKWARD>
-__global__ __launch_bounds__(S::WAVES * 64) void int8_tile_kernel(const TileParams a)
+template <typename S, int MATS, bool BACKWARD, int ACT>
+__global__ __launch_bounds__(S::WAVES * 64, 2) void int8_tile_kernel(const TileParams a)
 {
     using L = TileLds<S, MATS, BACKWARD>;
     constexpr int FRC = S::FR / MATS;                       // tiles of 32 channels in a wave
@@ -81,7 +109,8 @@ __global__ __launch_bounds__(S::WAVES * 64) void int8_tile_kernel(const TilePara
     static_assert(!BACKWARD || CHANNELS % 64 == 0, "the last tile writes the gradients' rows to their end");
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wr = wave / S::WT, wt = wave % S::WT;
+    const int team = wave / S::TEAM_WAVES, tw = wave % S::TEAM_WAVES;
+    const int wr = tw / S::WT, wt = tw % S::WT;
     const int r32 = lane & 31, half = lane >> 5;
 
     // the tile: first by XCD, then in groups of up to eight token tiles, the tokens of a group running fastest
@@ -97,44 +126,59 @@ __global__ __launch_bounds__(S::WAVES * 64) void int8_tile_kernel(const TilePara
     const int8_t *const q_base = a.q + (int64_t)t0 * a.n;
     const int8_t *const w_base = a.w[0] + (int64_t)ch0 * a.n, *const u_base = a.w[MATS - 1] + (int64_t)ch0 * a.n;
 
-    // Load k of a stage brings 1 KiB: LDS rows 8k .. 8k+7; lane l delivers the part that belongs at place l % 8 of row 8k + l / 8.
+    // A load brings 1 KiB: LOAD_ROWS rows; lane l delivers the part that belongs at place l % PLACES of row l / PLACES of them.
     // Rows and tokens past the end repeat the last one (their results are not stored).
-    constexpr int W_LOADS = S::ROWS / 8 / S::WAVES, Q_LOADS = S::TOKS / 8 / S::WAVES;
-    static_assert(W_LOADS * 8 * S::WAVES == S::ROWS && Q_LOADS * 8 * S::WAVES == S::TOKS, "whole loads per wave");
+    constexpr int W_LOADS = S::ROWS / S::LOAD_ROWS / S::TEAM_WAVES, Q_LOADS = S::TOKS / S::LOAD_ROWS / S::TEAM_WAVES;
+    static_assert(W_LOADS * S::LOAD_ROWS * S::TEAM_WAVES == S::ROWS && Q_LOADS * S::LOAD_ROWS * S::TEAM_WAVES == S::TOKS, "whole loads per wave");
     uint32_t w_src[W_LOADS], q_src[Q_LOADS], w_part[W_LOADS], q_part[Q_LOADS];
 #pragma unroll
     for (int k = 0; k < W_LOADS; ++k) {
-        const uint32_t row = 8 * (wave * W_LOADS + k) + (lane >> 3);
-        w_part[k] = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+        const uint32_t row = S::LOAD_ROWS * (tw * W_LOADS + k) + lane / S::PLACES;
+        w_part[k] = (lane % S::PLACES ^ S::swizzle(row)) * 16;
         const uint32_t in_wave = row % (S::FR * 32);
         const uint32_t ch = MATS == 1 ? row : row / (S::FR * 32) * (FRC * 32) + in_wave % (FRC * 32);
         w_src[k] = min(ch, chs - 1) * a.n;
     }
 #pragma unroll
     for (int k = 0; k < Q_LOADS; ++k) {
-        const uint32_t tok = 8 * (wave * Q_LOADS + k) + (lane >> 3);
-        q_part[k] = ((lane & 7) ^ ((tok >> 1) & 7)) * 16;
+        const uint32_t tok = S::LOAD_ROWS * (tw * Q_LOADS + k) + lane / S::PLACES;
+        q_part[k] = (lane % S::PLACES ^ S::swizzle(tok)) * 16;
         q_src[k] = min(tok, toks - 1) * a.n;
     }
-    // Columns k0 .. k0+127 into a buffer.  In the last step parts past the row's end bring the row's first part instead: what is
+    // The backward pass's tile of dy, asked for before everything else (at the end nothing would hide its way).
+    constexpr int PIECES = CHANNELS / 8, THREADS = S::WAVES * 64;           // 16-byte pieces of a tile's row
+    [[maybe_unused]] u32x4 dy_early[BACKWARD ? L::DY_EACH : 1];
+    if constexpr (BACKWARD) {
+        static_assert(L::DY_EACH * THREADS == S::TOKS * PIECES && S::TOKS * CHANNELS % (8 * THREADS) == 0, "the same for every thread");
+        if (a.whole) {
+#pragma unroll
+            for (int k = 0; k < L::DY_EACH; ++k) {
+                const uint32_t tok = (threadIdx.x + k * THREADS) / PIECES, piece = (threadIdx.x + k * THREADS) % PIECES;
+                dy_early[k] = tok < toks && piece * 8 < chs ? *reinterpret_cast<const u32x4 *>(a.dy + (int64_t)(t0 + tok) * a.m + ch0 + piece * 8) : u32x4{0, 0, 0, 0};
+            }
+        }
+    }
+
+    unsigned char *const mine = lds + team * S::RING * L::STAGE;        // the team's ring
+    // Columns k0 .. k0 + STEP - 1 into a buffer.  In the last step parts past the row's end bring the row's first part instead: what is
     // multiplied with them is set to zero.
     auto stage = [&](int buffer, uint32_t k0) {
-        unsigned char *to = lds + buffer * L::STAGE;
-        const bool last = k0 + kStep > a.n;
+        unsigned char *to = mine + buffer * L::STAGE;
+        const bool last = k0 + S::STEP > a.n;
         const auto q_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(q_base), 0, (int)(toks * a.n), 0x00020000);
         auto column = [&](uint32_t part) { return last && k0 + part >= a.n ? 0u : k0 + part; };
 #pragma unroll
         for (int k = 0; k < W_LOADS; ++k) {
-            const int unit = wave * W_LOADS + k;
-            const bool up = MATS == 2 && (unit * 8) % (S::FR * 32) >= FRC * 32;
+            const int unit = tw * W_LOADS + k;
+            const bool up = MATS == 2 && (unit * S::LOAD_ROWS) % (S::FR * 32) >= FRC * 32;
             const auto w_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(up ? u_base : w_base), 0, (int)(chs * a.n), 0x00020000);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(w_rsrc, (__attribute__((address_space(3))) void *)(to + unit * 1024), 16,
                                                      (int)(w_src[k] + column(w_part[k])), 0, 0, 0);
         }
 #pragma unroll
         for (int k = 0; k < Q_LOADS; ++k) {
-            const int unit = wave * Q_LOADS + k;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(q_rsrc, (__attribute__((address_space(3))) void *)(to + S::ROWS * kStep + unit * 1024), 16,
+            const int unit = tw * Q_LOADS + k;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(q_rsrc, (__attribute__((address_space(3))) void *)(to + S::ROWS * S::STEP + unit * 1024), 16,
                                                      (int)(q_src[k] + column(q_part[k])), 0, 0, 0);
         }
     };
@@ -147,38 +191,115 @@ __global__ __launch_bounds__(S::WAVES * 64) void int8_tile_kernel(const TilePara
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[r][t][i] = 0;
 
-    const uint32_t swz = (r32 >> 1) & 7;
-    auto multiply = [&](int buffer, int kk, bool there) {
-        const unsigned char *from = lds + buffer * L::STAGE + r32 * kStep + (((2 * kk + half) ^ swz) << 4);
+    const uint32_t swz = S::swizzle(r32);
+    struct Operands {
         v4i w[S::FR], x[S::FT];
+    };
+    auto operands = [&](int buffer, int kk) {
+        const unsigned char *from = mine + buffer * L::STAGE + r32 * S::STEP + (((2 * kk + half) ^ swz) << 4);
+        Operands o;
 #pragma unroll
-        for (int r = 0; r < S::FR; ++r) w[r] = *reinterpret_cast<const v4i *>(from + (wr * S::FR + r) * 32 * kStep);
+        for (int r = 0; r < S::FR; ++r) o.w[r] = *reinterpret_cast<const v4i *>(from + (wr * S::FR + r) * 32 * S::STEP);
 #pragma unroll
-        for (int t = 0; t < S::FT; ++t) {
-            x[t] = *reinterpret_cast<const v4i *>(from + S::ROWS * kStep + (wt * S::FT + t) * 32 * kStep);
-            if (!there) x[t] = v4i{0, 0, 0, 0};
-        }
+        for (int t = 0; t < S::FT; ++t) o.x[t] = *reinterpret_cast<const v4i *>(from + S::ROWS * S::STEP + (wt * S::FT + t) * 32 * S::STEP);
+        return o;
+    };
+    auto multiply = [&](const Operands &o) {
 #pragma unroll
         for (int r = 0; r < S::FR; ++r)
 #pragma unroll
-            for (int t = 0; t < S::FT; ++t) acc[r][t] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[r], x[t], acc[r][t], 0, 0, 0);
+            for (int t = 0; t < S::FT; ++t) acc[r][t] = __builtin_amdgcn_mfma_i32_32x32x32_i8(o.w[r], o.x[t], acc[r][t], 0, 0, 0);
+    };
+    // One step.  ACROSS: its first operands are there, and each time the next operands are read between the matrix instructions, at the end those of
+    // the step in buffer `after`.
+    [[maybe_unused]] Operands now;
+    auto whole_step = [&](int buffer, int after) {
+#pragma unroll
+        for (int kk = 0; kk < S::STEP / 32; ++kk) {
+            if constexpr (S::ACROSS) {
+                const Operands later = kk + 1 < S::STEP / 32 ? operands(buffer, kk + 1) : operands(after, 0);
+                multiply(now);
+                now = later;
+                constexpr int READS = S::FR + S::FT, PRODUCTS = S::FR * S::FT;
+#pragma unroll
+                for (int i = 0; i < (READS > PRODUCTS ? READS : PRODUCTS); ++i) {
+                    if (i < READS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    if (i < PRODUCTS) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                }
+            } else {
+                multiply(operands(buffer, kk));
+            }
+        }
     };
 
-    const int steps = (int)(a.n / kStep), tail = (int)(a.n % kStep);
+    const int steps = (int)(a.n / S::STEP), tail = (int)(a.n % S::STEP);
     const int stages = steps + (tail ? 1 : 0);
-    stage(0, 0);
-    for (int s = 0; s < steps; ++s) {
-        // this step's tiles have landed, and nobody reads the other buffer any more
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (s + 1 < stages) stage((s + 1) & 1, (uint32_t)(s + 1) * kStep);
+    // The teams take the steps by turns: round i is step i TEAMS + team, in buffer i % RING.  At the top of a round its tiles and the next
+    // one's have landed, what later rounds asked for is still under way, and nobody reads the buffer of the round before any more, into which the
+    // round RING - 1 ahead then goes.  (A team may have no step in the last round, and nothing else is missing.)
+    constexpr int AHEAD = S::RING - 1, LOADS = W_LOADS + Q_LOADS;
+    static_assert(S::RING >= 3 || !S::ACROSS, "a step reads the next one's first operands");
+    const int rounds = (stages + S::TEAMS - 1) / S::TEAMS;
+    auto step = [&](int i) { return i * S::TEAMS + team; };
+    for (int i = 0; i < min(AHEAD, rounds); ++i)
+        if (step(i) < stages) stage(i, (uint32_t)step(i) * S::STEP);
+    if (rounds > AHEAD) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((AHEAD - 1) * LOADS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    if (S::ACROSS) now = operands(0, 0);
+    int buffer = 0, into = AHEAD, i = 0;
+    auto next = [](int b) { return b + 1 == S::RING ? 0 : b + 1; };
+    for (; i + AHEAD < rounds; ++i) {                       // (whole steps: the last one is still to come)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD - (S::ACROSS ? 2 : 1)) * LOADS) : "memory");
+        if (S::TEAMS == 1 || step(i + AHEAD) < stages) stage(into, (uint32_t)step(i + AHEAD) * S::STEP);
+        whole_step(buffer, next(buffer));
+        buffer = next(buffer);
+        into = next(into);
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    for (; step(i) < steps; ++i) {                          // (behind the last step, what is read for the next one is nothing)
+        whole_step(buffer, next(buffer));
+        buffer = next(buffer);
+    }
+    if (step(i) < stages)
+        for (int kk = 0; kk * 32 < tail; ++kk) {
+            Operands o = operands(buffer, kk);
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) multiply(s & 1, kk, true);
-    }
-    if (tail) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        for (int kk = 0; kk * 32 < tail; ++kk) multiply(steps & 1, kk, kk * 32 + half * 16 < tail);
-    }
+            for (int t = 0; t < S::FT; ++t)
+                if (kk * 32 + half * 16 >= tail) o.x[t] = v4i{0, 0, 0, 0};
+            multiply(o);
+        }
     __syncthreads();
+    // the other teams' sums to the first
+    if constexpr (S::TEAMS > 1) {
+        v4i *const exchange = reinterpret_cast<v4i *>(lds) + tw * (S::FR * S::FT * 4 * 64) + lane;
+        constexpr int BETWEEN = S::TEAM_WAVES * S::FR * S::FT * 4 * 64;
+        if (team > 0) {
+#pragma unroll
+            for (int r = 0; r < S::FR; ++r)
+#pragma unroll
+                for (int t = 0; t < S::FT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        exchange[(team - 1) * BETWEEN + ((r * S::FT + t) * 4 + e) * 64] =
+                            v4i{acc[r][t][4 * e], acc[r][t][4 * e + 1], acc[r][t][4 * e + 2], acc[r][t][4 * e + 3]};
+        }
+        __syncthreads();
+        if (team == 0) {
+#pragma unroll
+            for (int k = 0; k < S::TEAMS - 1; ++k)
+#pragma unroll
+                for (int r = 0; r < S::FR; ++r)
+#pragma unroll
+                    for (int t = 0; t < S::FT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const v4i v = exchange[k * BETWEEN + ((r * S::FT + t) * 4 + e) * 64];
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) acc[r][t][4 * e + c] += v[c];
+                        }
+        }
+        __syncthreads();
+    }
 
     // the channels' and tokens' scales, and in the backward pass the tile of dy
     float *scales = reinterpret_cast<float *>(lds + L::SCALES);
@@ -189,23 +310,27 @@ __global__ __launch_bounds__(S::WAVES * 64) void int8_tile_kernel(const TilePara
     float *token_scales = reinterpret_cast<float *>(lds + L::TOKEN_SCALES);
     [[maybe_unused]] float *norms = token_scales + S::TOKS;
     for (uint32_t i = threadIdx.x; i < S::TOKS; i += S::WAVES * 64) {
-        token_scales[i] = a.token_scales[t0 + min(i, toks - 1)];
-        if constexpr (BACKWARD) norms[i] = a.norms[t0 + min(i, toks - 1)];
+        token_scales[i] = i < toks ? a.token_scales[t0 + i] : 0.f;
+        if constexpr (BACKWARD) norms[i] = i < toks ? a.norms[t0 + i] : 1.f;
     }
-    constexpr int PIECES = CHANNELS / 8;                    // 16-byte pieces of a tile's row
     if constexpr (BACKWARD) {
         if (a.whole) {
-            for (int i = threadIdx.x; i < S::TOKS * PIECES; i += S::WAVES * 64) {
-                const uint32_t tok = i / PIECES, piece = i % PIECES;
-                u32x4 v = {0, 0, 0, 0};
-                if (tok < toks && piece * 8 < chs) v = *reinterpret_cast<const u32x4 *>(a.dy + (int64_t)(t0 + tok) * a.m + ch0 + piece * 8);
-                *reinterpret_cast<u32x4 *>(lds + tok * L::OUT_ROW + piece * 16) = v;
+#pragma unroll
+            for (int k = 0; k < L::DY_EACH; ++k) {
+                const uint32_t i = threadIdx.x + k * THREADS;
+                *reinterpret_cast<u32x4 *>(lds + i / PIECES * L::OUT_ROW + i % PIECES * 16) = dy_early[k];
             }
         } else {
-            for (int i = threadIdx.x; i < S::TOKS * CHANNELS; i += S::WAVES * 64) {
-                const uint32_t tok = i / CHANNELS, ch = i % CHANNELS;
-                *reinterpret_cast<uint16_t *>(lds + tok * L::OUT_ROW + ch * 2) =
-                    tok < toks && ch < chs ? a.dy[(int64_t)(t0 + tok) * a.m + ch0 + ch] : (uint16_t)0;
+            for (int i = threadIdx.x; i < S::TOKS * CHANNELS; i += 8 * THREADS) {
+                uint16_t v[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint32_t tok = (i + k * THREADS) / CHANNELS, ch = (i + k * THREADS) % CHANNELS;
+                    v[k] = tok < toks && ch < chs ? a.dy[(int64_t)(t0 + tok) * a.m + ch0 + ch] : (uint16_t)0;
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    *reinterpret_cast<uint16_t *>(lds + (i + k * THREADS) / CHANNELS * L::OUT_ROW + (i + k * THREADS) % CHANNELS * 2) = v[k];
             }
         }
     }
@@ -216,74 +341,76 @@ __global__ __launch_bounds__(S::WAVES * 64) void int8_tile_kernel(const TilePara
     // 32 sums over this wave's tokens at a time: a tile of channels of each matrix, or two tiles of the one
     constexpr int TOGETHER = BACKWARD && MATS == 1 ? 2 : 1;
     static_assert(FRC % TOGETHER == 0, "whole exchanges");
+    auto results = [&] {
 #pragma unroll
-    for (int r0 = 0; r0 < FRC; r0 += TOGETHER) {
-        [[maybe_unused]] float sums[32];
-        if constexpr (BACKWARD)
+        for (int r0 = 0; r0 < FRC; r0 += TOGETHER) {
+            [[maybe_unused]] float sums[32];
+            if constexpr (BACKWARD)
 #pragma unroll
-            for (int i = 0; i < 32; ++i) sums[i] = 0.f;
+                for (int i = 0; i < 32; ++i) sums[i] = 0.f;
 #pragma unroll
-        for (int r = r0; r < r0 + TOGETHER; ++r)
+            for (int r = r0; r < r0 + TOGETHER; ++r)
 #pragma unroll
-            for (int t = 0; t < S::FT; ++t) {
-                const uint32_t tok = (wt * S::FT + t) * 32 + r32;
-                const float ts = token_scales[tok];
-                [[maybe_unused]] float norm = 0.f;
-                if constexpr (BACKWARD) norm = norms[tok];
-                const bool here = tok < toks;
+                for (int t = 0; t < S::FT; ++t) {
+                    const uint32_t tok = (wt * S::FT + t) * 32 + r32;
+                    const float ts = token_scales[tok];
+                    [[maybe_unused]] float norm = 0.f;
+                    if constexpr (BACKWARD) norm = norms[tok];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int ch = (wr * FRC + r) * 32 + 8 * e + 4 * half;     // element 4 e + i: channel ch + i
-                    unsigned char *at = lds + tok * L::OUT_ROW + ch * 2;
-                    const v4f c0 = *reinterpret_cast<const v4f *>(scales + ch);
-                    const v4f c1 = *reinterpret_cast<const v4f *>(scales + (MATS - 1) * CHANNELS + ch);
-                    [[maybe_unused]] u32x2 dy = {0, 0};
-                    if constexpr (BACKWARD) dy = *reinterpret_cast<const u32x2 *>(at);
-                    uint32_t out[4], out2[4];
+                    for (int e = 0; e < 4; ++e) {
+                        const int ch = (wr * FRC + r) * 32 + 8 * e + 4 * half;     // element 4 e + i: channel ch + i
+                        unsigned char *at = lds + tok * L::OUT_ROW + ch * 2;
+                        const v4f c0 = *reinterpret_cast<const v4f *>(scales + ch);
+                        const v4f c1 = *reinterpret_cast<const v4f *>(scales + (MATS - 1) * CHANNELS + ch);
+                        [[maybe_unused]] u32x2 dy = {0, 0};
+                        if constexpr (BACKWARD) dy = *reinterpret_cast<const u32x2 *>(at);
+                        uint32_t out[4], out2[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float p = (float)acc[r][t][4 * e + i] * ts;
-                        [[maybe_unused]] float p2 = 0.f, slope = 0.f;
-                        if constexpr (MATS == 2) p2 = (float)acc[FRC + r][t][4 * e + i] * ts;
-                        if constexpr (!BACKWARD) {
-                            float v = p * c0[i];
-                            if constexpr (MATS == 2) v = activate<false>(v, a.activation, slope) * (p2 * c1[i]);
-                            out[i] = to_16(v, a.bf16);
-                        } else {
-                            const float d = from_16((i & 1) ? dy[i >> 1] >> 16 : dy[i >> 1] & 0xffffu, a.bf16);
-                            const bool inside = here && (uint32_t)(ch + i) < chs;
-                            // The gradients that the second half multiplies are held in binary16 (11 bits): a token's by the power of two
-                            // that brings its largest dy to about 1/32, times its channel's scale over the power of two above all
-                            // scales, so that neither the type's range nor the scales' sizes matter.  A value is off by 2^-12 of
-                            // itself, as much as by a result's last rounding.
-                            const float k0 = norm * (c0[i] * inv_top);
-                            if constexpr (MATS == 1) {
-                                out[i] = inside ? to_16(d * k0, false) : 0u;
-                                sums[(r - r0) * 16 + 4 * e + i] += inside ? d * p : 0.f;
+                        for (int i = 0; i < 4; ++i) {
+                            const float p = (float)acc[r][t][4 * e + i] * ts;
+                            [[maybe_unused]] float p2 = 0.f, slope = 0.f;
+                            if constexpr (MATS == 2) p2 = (float)acc[FRC + r][t][4 * e + i] * ts;
+                            if constexpr (!BACKWARD) {
+                                float v = p * c0[i];
+                                if constexpr (MATS == 2) v = activate<false>(v, ACT, slope) * (p2 * c1[i]);
+                                out[i] = to_16(v, a.bf16);
                             } else {
-                                const float act = activate<true>(p * c0[i], a.activation, slope);
-                                const float dg = d * (p2 * c1[i]) * slope, du = d * act;
-                                out[i] = inside ? to_16(dg * k0, false) : 0u;
-                                out2[i] = inside ? to_16(du * (norm * (c1[i] * inv_top)), false) : 0u;
-                                sums[4 * e + i] += inside ? dg * p : 0.f;
-                                sums[16 + 4 * e + i] += inside ? du * p2 : 0.f;
+                                // (channels and tokens past the end have a gradient and a scale of 0)
+                                const float d = from_16((i & 1) ? dy[i >> 1] >> 16 : dy[i >> 1] & 0xffffu, a.bf16);
+                                // The gradients that the second half multiplies are held in binary16 (11 bits): a token's by the power of
+                                // two that brings its largest dy to about 1/32, times its channel's scale over the power of two above
+                                // all scales, so that neither the type's range nor the scales' sizes matter.  A value is off by
+                                // 2^-12 of itself, as much as by a result's last rounding.
+                                if constexpr (MATS == 1) {
+                                    out[i] = to_16(d * (norm * (c0[i] * inv_top)), false);
+                                    sums[(r - r0) * 16 + 4 * e + i] += d * p;
+                                } else {
+                                    const float act = activate<true>(p * c0[i], ACT, slope);
+                                    const float dg = d * (p2 * c1[i]) * slope, du = d * act;
+                                    out[i] = to_16(dg * (norm * (c0[i] * inv_top)), false);
+                                    out2[i] = to_16(du * (norm * (c1[i] * inv_top)), false);
+                                    sums[4 * e + i] += dg * p;
+                                    sums[16 + 4 * e + i] += du * p2;
+                                }
                             }
                         }
+                        *reinterpret_cast<u32x2 *>(at) = u32x2{out[0] | out[1] << 16, out[2] | out[3] << 16};
+                        if constexpr (BACKWARD && MATS == 2)
+                            *reinterpret_cast<u32x2 *>(at + L::OUT) = u32x2{out2[0] | out2[1] << 16, out2[2] | out2[3] << 16};
+                        if constexpr (BACKWARD) __builtin_amdgcn_sched_barrier(0);      // (four elements at a time: registers)
                     }
-                    *reinterpret_cast<u32x2 *>(at) = u32x2{out[0] | out[1] << 16, out[2] | out[3] << 16};
-                    if constexpr (BACKWARD && MATS == 2)
-                        *reinterpret_cast<u32x2 *>(at + L::OUT) = u32x2{out2[0] | out2[1] << 16, out2[2] | out2[3] << 16};
                 }
+            if constexpr (BACKWARD) {
+                // lane l of a half gets value l: element l % 16 of the first or second sixteen
+                const float sum = sums_of_32(sums, lane);
+                const int second = r32 >> 4, e = (r32 >> 2) & 3, i = r32 & 3;
+                const uint32_t ch = (wr * FRC + r0 + (MATS == 1 ? second : 0)) * 32 + 8 * e + 4 * half + i;
+                float *parts = a.parts + (int64_t)(token_tile * S::WT + wt) * MATS * a.m;
+                if (ch < chs) parts[(int64_t)(MATS == 1 ? 0 : second) * a.m + ch0 + ch] = sum;
             }
-        if constexpr (BACKWARD) {
-            // lane l of a half gets value l: element l % 16 of the first or second sixteen
-            const float sum = sums_of_32(sums, lane);
-            const int second = r32 >> 4, e = (r32 >> 2) & 3, i = r32 & 3;
-            const uint32_t ch = (wr * FRC + r0 + (MATS == 1 ? second : 0)) * 32 + 8 * e + 4 * half + i;
-            float *parts = a.parts + (int64_t)(token_tile * S::WT + wt) * MATS * a.m;
-            if (ch < chs) parts[(int64_t)(MATS == 1 ? 0 : second) * a.m + ch0 + ch] = sum;
         }
-    }
+    };
+    if (team == 0) results();
     __syncthreads();
 
     if constexpr (!BACKWARD) {
@@ -311,32 +438,61 @@ __global__ __launch_bounds__(S::WAVES * 64) void int8_tile_kernel(const TilePara
     }
 }
 
-template <typename S, int MATS, bool BACKWARD>
+template <typename S, int MATS, bool BACKWARD, int ACT>
 hipError_t go(TileParams p, hipStream_t stream, int64_t *part_count)
 {
     using L = TileLds<S, MATS, BACKWARD>;
     p.row_tiles = (p.m + L::CHANNELS - 1) / L::CHANNELS;
     p.token_tiles = (p.tokens + S::TOKS - 1) / S::TOKS;
     if (part_count) *part_count = (int64_t)p.token_tiles * S::WT;
-    const auto kernel = int8_tile_kernel<S, MATS, BACKWARD>;
+    const auto kernel = int8_tile_kernel<S, MATS, BACKWARD, ACT>;
     if (hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), L::BYTES)) return e;
     hipLaunchKernelGGL(kernel, dim3(p.row_tiles * p.token_tiles), dim3(S::WAVES * 64), L::BYTES, stream, p);
     return hipGetLastError();
 }
 
-using Large = TileShape<2, 4, 4, 2>;        // 256 x 256
-using Medium = TileShape<2, 2, 2, 2>;       // 128 x 128
-// 64 x 64; in the gated backward pass 128 x 64, so that its channels are a multiple of 64 as the gradients' rows are
-template <int MATS, bool BACKWARD> using Small = TileShape<BACKWARD && MATS == 2 ? 2 : 1, 2, 2, 1>;
+// What a workgroup takes per 128 columns where the chip is full, alone on its CU and, where two fit, beside a second one (microseconds, measured):
+// the shape that is expected to be done first is taken.  Large tiles read each operand from the caches the fewest times; small ones, with teams or a
+// deep ring, give every CU work and keep enough bytes under way where there are few.
+template <int MATS, bool BACKWARD, typename F>
+void for_shapes(F f)
+{
+    // (the gated backward pass: a multiple of 64 channels, as the gradients' rows are)
+    constexpr int ROW_WAVES = BACKWARD && MATS == 2 ? 2 : 1;
+    f(TileShape<2, 4, 4, 2, 2>{}, 1.70f, 0.f);                                      // 256 x 256
+    f(TileShape<4, 2, 2, 2, 3>{}, 1.20f, 0.f);                                      // 256 x 128
+    f(TileShape<2, 2, 2, 2, 2>{}, 0.72f, 1.12f);                                    // 128 x 128, two on a CU
+    f(TileShape<2, 2, 2, 2, 4>{}, 0.60f, 0.f);                                      // 128 x 128
+    f(TileShape<ROW_WAVES, 2, 2, 1, ROW_WAVES == 2 ? 3 : 4>{}, ROW_WAVES * 0.37f, ROW_WAVES * 0.48f);          // 64 x 64 (128 x 64), two on a CU
+    f(TileShape<ROW_WAVES, 2, 2, 1, ROW_WAVES == 2 ? 3 : 4, 2>{}, ROW_WAVES * 0.28f, 0.f);                     // 64 x 64 (128 x 64), two teams
+}
 
-// The largest tile that leaves no CU without one.
 template <int MATS, bool BACKWARD>
 hipError_t pick(const TileParams &p, hipStream_t stream, int64_t *part_count = nullptr)
 {
-    auto tiles = [&](int rows, int toks) { return (int64_t)((p.m * MATS + rows - 1) / rows) * ((p.tokens + toks - 1) / toks); };
-    if (tiles(256, 256) >= 256) return go<Large, MATS, BACKWARD>(p, stream, part_count);
-    if (tiles(128, 128) >= 256) return go<Medium, MATS, BACKWARD>(p, stream, part_count);
-    return go<Small<MATS, BACKWARD>, MATS, BACKWARD>(p, stream, part_count);
+    float best = 0.f;
+    int index = 0, chosen = -1;
+    for_shapes<MATS, BACKWARD>([&](auto shape, float alone, float beside) {
+        using S = decltype(shape);
+        const int64_t tiles = (int64_t)((p.m * MATS + S::ROWS - 1) / S::ROWS) * ((p.tokens + S::TOKS - 1) / S::TOKS);
+        const int64_t each = (tiles + 255) / 256;                   // tiles of the busiest CU
+        const float us = beside > 0.f ? (float)(each / 2) * beside + (float)(each % 2) * alone : (float)each * alone;
+        if (chosen < 0 || us < best) {
+            best = us;
+            chosen = index;
+        }
+        ++index;
+    });
+    hipError_t result = hipErrorInvalidValue;
+    index = 0;
+    for_shapes<MATS, BACKWARD>([&](auto shape, float, float) {
+        if (index++ == chosen) {
+            using S = decltype(shape);
+            if (MATS == 2 && p.activation == BCQ_ACT_GELU) result = go<S, MATS, BACKWARD, MATS == 2 ? BCQ_ACT_GELU : BCQ_ACT_SILU>(p, stream, part_count);
+            else result = go<S, MATS, BACKWARD, BCQ_ACT_SILU>(p, stream, part_count);
+        }
+    });
+    return result;
 }
 
 TileParams params(const Int8Args &a)

@@ -74,21 +74,21 @@ def test_gated(lib):
 
 def test_workspace(lib):
     size = lib.bcq_int8_backward_workspace
-    assert size(1, 8, 0) >= 0
+    assert size(1, 8, 64, 0) >= 0
     for matrices in (0, 3):
-        assert size(matrices, 8, 4) == SHAPE
-    for m, tokens in ((0, 4), ((1 << 20) + 1, 4), (8, -1), (8, (1 << 24) + 1)):
-        assert size(1, m, tokens) == SHAPE
+        assert size(matrices, 8, 64, 4) == SHAPE
+    for m, n, tokens in [*BAD_SHAPES, ((1 << 20) + 1, 64, 4)]:
+        assert size(1, m, n, tokens) == SHAPE
     # the gradients of the projections in 16 bits at least, and growing with what it holds
-    assert size(1, 1000, 100) >= 2 * 1000 * 100
-    assert size(2, 1000, 100) >= 2 * 2 * 1000 * 100
-    assert size(2, 14336, 4096) > size(1, 14336, 4096) > size(1, 14336, 4095)
-    assert size(2, 1 << 20, 1 << 20) > 1 << 42
+    assert size(1, 1000, 64, 100) >= 2 * 1000 * 100
+    assert size(2, 1000, 64, 100) >= 2 * 2 * 1000 * 100
+    assert size(2, 14336, 64, 4096) > size(1, 14336, 64, 4096) > size(1, 14336, 64, 4095)
+    assert size(2, 1 << 20, 64, 1 << 20) > 1 << 42
 
 
 def test_gemm_backward(lib):
     f = lib.bcq_int8_gemm_backward
-    need = lib.bcq_int8_backward_workspace(1, 8, 4)
+    need = lib.bcq_int8_backward_workspace(1, 8, 64, 4)
     args = dict(dy=Y, q=Q, ts=TS, w=W, cs=CS, dx=0x6000, dcs=0x7000, type=F16, m=8, n=64, tokens=4, ws=WS, size=need - 1, stream=None)
     assert f(*args.values()) == WORKSPACE
     args["size"] = need
@@ -103,7 +103,7 @@ def test_gemm_backward(lib):
 
 def test_gated_backward(lib):
     f = lib.bcq_int8_gated_backward
-    need = lib.bcq_int8_backward_workspace(2, 8, 4)
+    need = lib.bcq_int8_backward_workspace(2, 8, 64, 4)
     args = dict(dh=Y, q=Q, ts=TS, wg=W, cg=CS, wu=W + 0x100, cu=CS + 0x100, activation=0, dx=0x6000, dg=0x7000, du=0x8000, type=F16, m=8, n=64,
                 tokens=4, ws=WS, size=need - 1, stream=None)
     assert f(*args.values()) == WORKSPACE
