@@ -37,6 +37,7 @@ class BcqError(RuntimeError):
 class _NoHost:
     """In the place of ``_bcq_host``: declines every call, so that the Python code makes it."""
     gemv = gemv_multi = gemm_mixed = int8_quantize = int8_gemm = int8_gated = staticmethod(lambda *args: None)
+    int8_gemm_backward = int8_gated_backward = staticmethod(lambda *args: None)
 
 
 def _load_host(functions, int8_functions):
@@ -107,7 +108,8 @@ def lib() -> ctypes.CDLL:
         for f in (L.bcq_int8_quantize, L.bcq_int8_gemm, L.bcq_int8_gated, L.bcq_int8_gemm_backward, L.bcq_int8_gated_backward):
             f.restype = i32
         _host = _load_host((L.bcq_gemv_offset, L.bcq_gemv_multi, L.bcq_gemm_mixed, L.bcq_gemm_mixed_offset),
-                           (L.bcq_int8_quantize, L.bcq_int8_gemm, L.bcq_int8_gated))
+                           (L.bcq_int8_quantize, L.bcq_int8_gemm, L.bcq_int8_gated, L.bcq_int8_backward_workspace, L.bcq_int8_gemm_backward,
+                            L.bcq_int8_gated_backward))
         _lib = L
     return _lib
 
@@ -449,7 +451,11 @@ def bcq_int8_gemm_backward(dy: torch.Tensor, q: torch.Tensor, token_scales: torc
     """Gradients of ``bcq_int8_gemm`` with the codes fixed: ``(dx [tokens][n] of dy's type, dchannel_scales float32 [m])``, dx being the
     gradient of the activations that were quantised."""
     where = "bcq_int8_gemm_backward"
-    lib()
+    if _host is None:
+        lib()
+    done = _host.int8_gemm_backward(dy, q, token_scales, w, channel_scales)
+    if done is not None:
+        return done
     tokens, m, n = _int8_shapes(where, q, token_scales, [(w, channel_scales)])
     with torch.cuda.device(q.device):
         kind, dx, size, workspace = _int8_backward_setup(where, dy, tokens, m, n, 1, q)
@@ -465,7 +471,11 @@ def bcq_int8_gated_backward(dh: torch.Tensor, q: torch.Tensor, token_scales: tor
     """Gradients of ``bcq_int8_gated`` with the codes fixed: ``(dx [tokens][n] of dh's type, dgate_scales float32 [m], dup_scales float32
     [m])``; the projections are computed again."""
     where = "bcq_int8_gated_backward"
-    lib()
+    if _host is None:
+        lib()
+    done = _host.int8_gated_backward(dh, q, token_scales, w_gate, gate_scales, w_up, up_scales, activation)
+    if done is not None:
+        return done
     tokens, m, n = _int8_shapes(where, q, token_scales, [(w_gate, gate_scales), (w_up, up_scales)])
     act = _activation(activation, where)
     with torch.cuda.device(q.device):

@@ -26,6 +26,9 @@ decltype(&bcq_gemm_mixed_offset) g_mixed_offset = nullptr;
 decltype(&bcq_int8_quantize) g_int8_quantize = nullptr;
 decltype(&bcq_int8_gemm) g_int8_gemm = nullptr;
 decltype(&bcq_int8_gated) g_int8_gated = nullptr;
+decltype(&bcq_int8_backward_workspace) g_int8_workspace = nullptr;
+decltype(&bcq_int8_gemm_backward) g_int8_gemm_backward = nullptr;
+decltype(&bcq_int8_gated_backward) g_int8_gated_backward = nullptr;
 PyObject *g_error = nullptr;            // the exception class: (status, where)
 
 // A plain tensor on the GPU, contiguous, of this type; nullptr otherwise.  (Subclasses, wrappers and tensors without storage go the Python way.)
@@ -372,14 +375,78 @@ PyObject *int8_gated(PyObject *, PyObject *const *a, Py_ssize_t count)
     });
 }
 
-// bind_int8(quantize, gemm, gated): likewise the 8-bit operators
+// What the backward calls share: the gradient, new results (dx, then the gradients of the scales, a tuple) and the workspace; the call itself is `f`'s.
+template <typename F>
+PyObject *int8_backward(PyObject *const *a, int mats, const char *where, F f)
+{
+    int type;
+    const at::Tensor *dy = gpu_tensor(a[0], at::kHalf), *t[6];
+    if (!dy) dy = gpu_tensor(a[0], at::kBFloat16);
+    if (!dy || !type_of(dy->scalar_type(), type)) Py_RETURN_NONE;
+    OneDevice on(*dy);
+    int64_t m, n, tokens;
+    if (!int8_operands(on, a + 1, mats, t, m, n, tokens) || !matrix_fits(dy, tokens, m)) Py_RETURN_NONE;
+    const int64_t size = g_int8_workspace(mats, m, n, tokens);
+    if (size < 0) Py_RETURN_NONE;
+    const at::Tensor workspace = output(*dy, {size}, at::kByte);
+    at::Tensor dx = output(*dy, {tokens, n}, dy->scalar_type()), dscales[2];
+    for (int k = 0; k < mats; ++k) dscales[k] = output(*dy, {m}, at::kFloat);
+    const int status = f(dy->const_data_ptr(), t, dx.mutable_data_ptr(), static_cast<float *>(dscales[0].mutable_data_ptr()),
+                         mats == 2 ? static_cast<float *>(dscales[1].mutable_data_ptr()) : nullptr, type, m, n, tokens, workspace.mutable_data_ptr(), size);
+    PyObject *results = PyTuple_New(1 + mats);
+    if (!results) return nullptr;
+    for (int k = 0; k <= mats; ++k) {
+        PyObject *r = THPVariable_Wrap(k == 0 ? std::move(dx) : std::move(dscales[k - 1]));
+        if (!r) {
+            Py_DECREF(results);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(results, k, r);
+    }
+    return finish(status, where, results);
+}
+
+// int8_gemm_backward(dy, q, token_scales, w, channel_scales) -> (dx, dchannel_scales)
+PyObject *int8_gemm_backward(PyObject *, PyObject *const *a, Py_ssize_t count)
+{
+    if (count != 5 || !g_int8_gemm_backward) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject * {
+        return int8_backward(a, 1, "bcq_int8_gemm_backward",
+                             [&](const void *dy, const at::Tensor **t, void *dx, float *d0, float *, int type, int64_t m, int64_t n, int64_t tokens,
+                                 void *workspace, int64_t size) {
+                                 return launch(g_int8_gemm_backward, dy, codes(t[0]), floats(t[1]), codes(t[2]), floats(t[3]), dx, d0, type, m, n, tokens,
+                                               workspace, size, stream());
+                             });
+    });
+}
+
+// int8_gated_backward(dh, q, token_scales, w_gate, gate_scales, w_up, up_scales, activation) -> (dx, dgate_scales, dup_scales)
+PyObject *int8_gated_backward(PyObject *, PyObject *const *a, Py_ssize_t count)
+{
+    if (count != 8 || !g_int8_gated_backward || !PyUnicode_CheckExact(a[7])) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject * {
+        const bool silu = PyUnicode_CompareWithASCIIString(a[7], "silu") == 0;
+        if (!silu && PyUnicode_CompareWithASCIIString(a[7], "gelu") != 0) Py_RETURN_NONE;
+        return int8_backward(a, 2, "bcq_int8_gated_backward",
+                             [&](const void *dh, const at::Tensor **t, void *dx, float *d0, float *d1, int type, int64_t m, int64_t n, int64_t tokens,
+                                 void *workspace, int64_t size) {
+                                 return launch(g_int8_gated_backward, dh, codes(t[0]), floats(t[1]), codes(t[2]), floats(t[3]), codes(t[4]), floats(t[5]),
+                                               (int)(silu ? BCQ_ACT_SILU : BCQ_ACT_GELU), dx, d0, d1, type, m, n, tokens, workspace, size, stream());
+                             });
+    });
+}
+
+// bind_int8(quantize, gemm, gated, backward_workspace, gemm_backward, gated_backward): likewise the 8-bit operators
 PyObject *bind_int8(PyObject *, PyObject *args)
 {
-    unsigned long long f[3];
-    if (!PyArg_ParseTuple(args, "KKK", &f[0], &f[1], &f[2])) return nullptr;
+    unsigned long long f[6];
+    if (!PyArg_ParseTuple(args, "KKKKKK", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5])) return nullptr;
     g_int8_quantize = reinterpret_cast<decltype(g_int8_quantize)>(f[0]);
     g_int8_gemm = reinterpret_cast<decltype(g_int8_gemm)>(f[1]);
     g_int8_gated = reinterpret_cast<decltype(g_int8_gated)>(f[2]);
+    g_int8_workspace = reinterpret_cast<decltype(g_int8_workspace)>(f[3]);
+    g_int8_gemm_backward = reinterpret_cast<decltype(g_int8_gemm_backward)>(f[4]);
+    g_int8_gated_backward = reinterpret_cast<decltype(g_int8_gated_backward)>(f[5]);
     Py_RETURN_NONE;
 }
 
@@ -404,6 +471,8 @@ PyMethodDef g_methods[] = {{"gemv", (PyCFunction)(void (*)(void))gemv, METH_FAST
                            {"int8_quantize", (PyCFunction)(void (*)(void))int8_quantize, METH_FASTCALL, nullptr},
                            {"int8_gemm", (PyCFunction)(void (*)(void))int8_gemm, METH_FASTCALL, nullptr},
                            {"int8_gated", (PyCFunction)(void (*)(void))int8_gated, METH_FASTCALL, nullptr},
+                           {"int8_gemm_backward", (PyCFunction)(void (*)(void))int8_gemm_backward, METH_FASTCALL, nullptr},
+                           {"int8_gated_backward", (PyCFunction)(void (*)(void))int8_gated_backward, METH_FASTCALL, nullptr},
                            {"bind", bind, METH_VARARGS, nullptr},
                            {"bind_int8", bind_int8, METH_VARARGS, nullptr},
                            {nullptr, nullptr, 0, nullptr}};

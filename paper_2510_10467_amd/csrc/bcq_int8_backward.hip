@@ -74,25 +74,7 @@ __global__ __launch_bounds__(256) void int8_norms_kernel(const uint16_t *__restr
     else norms[token] = ldexpf(1.f, usable ? -5 - e : 0);
 }
 
-// In the partial sums' order; eight are under way at a time.
-__global__ __launch_bounds__(64) void int8_sums_kernel(const float *__restrict__ parts, float *__restrict__ d0, float *__restrict__ d1, int64_t m,
-                                                       int matrices, int64_t part_count)
-{
-    const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x, stride = m * matrices;
-    if (i >= stride) return;
-    float sum = 0.f;
-    int64_t p = 0;
-    for (; p + 8 <= part_count; p += 8) {
-        float v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = parts[(p + k) * stride + i];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) sum += v[k];
-    }
-    for (; p < part_count; ++p) sum += parts[p * stride + i];
-    if (i < m) d0[i] = sum;
-    else d1[i - m] = sum;
-}
+constexpr uint32_t kTokenGroup = 4;       // token tiles whose workgroups run beside each other for a column tile
 
 struct SecondParams {
     const _Float16 *grad;
@@ -149,10 +131,10 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_second_kernel(const Sec
 
     const uint32_t total = gridDim.x, xcd = blockIdx.x & 7;
     const uint32_t id = xcd * (total >> 3) + min(xcd, total & 7) + (blockIdx.x >> 3);
-    const uint32_t group = id / (8 * a.column_tiles);
-    const uint32_t in_group = min(8u, a.token_tiles - group * 8);
-    const uint32_t rest = id - group * 8 * a.column_tiles;
-    const uint32_t c0 = rest / in_group * S::COLS, t0 = (group * 8 + rest % in_group) * S::TOKS;
+    const uint32_t group = id / (kTokenGroup * a.column_tiles);
+    const uint32_t in_group = min(kTokenGroup, a.token_tiles - group * kTokenGroup);
+    const uint32_t rest = id - group * kTokenGroup * a.column_tiles;
+    const uint32_t c0 = rest / in_group * S::COLS, t0 = (group * kTokenGroup + rest % in_group) * S::TOKS;
     const uint32_t cols = min((uint32_t)S::COLS, a.n - c0), toks = min((uint32_t)S::TOKS, a.tokens - t0);
 
     constexpr int W_LOADS = S::W_BYTES / 1024 / S::TEAM_WAVES, G_LOADS = S::TOKS / S::LOAD_TOKS / S::TEAM_WAVES;
@@ -354,20 +336,46 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_second_kernel(const Sec
     }
 }
 
-// The runs' sums, in order, to dx: four columns a thread.
-__global__ __launch_bounds__(256) void int8_splits_kernel(const float *__restrict__ split_sums, const float *__restrict__ norms,
-                                                          const float *__restrict__ scale_top, uint16_t *__restrict__ dx, int64_t tokens, uint32_t n,
-                                                          int splits, bool bf16)
+// What is left, in one launch: the first sums_blocks workgroups add up the partial sums of the scales' gradients, in order, a channel a thread and eight
+// under way at a time; the others the runs' sums of dx, four columns a thread.
+struct FinishParams {
+    const float *parts, *split_sums, *norms, *scale_top;
+    float *dscales[2];
+    uint16_t *dx;
+    int64_t m, part_count, tokens;
+    uint32_t n, sums_blocks;
+    int matrices, splits;
+    bool bf16;
+};
+
+__global__ __launch_bounds__(64) void int8_finish_kernel(const FinishParams a)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, count = tokens * n / 4;
+    if (blockIdx.x < a.sums_blocks) {
+        const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x, stride = a.m * a.matrices;
+        if (i >= stride) return;
+        float sum = 0.f;
+        int64_t p = 0;
+        for (; p + 8 <= a.part_count; p += 8) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = a.parts[(p + k) * stride + i];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += v[k];
+        }
+        for (; p < a.part_count; ++p) sum += a.parts[p * stride + i];
+        if (i < a.m) a.dscales[0][i] = sum;
+        else a.dscales[1][i - a.m] = sum;
+        return;
+    }
+    const int64_t i = (int64_t)(blockIdx.x - a.sums_blocks) * 64 + threadIdx.x, count = a.tokens * a.n / 4;
     if (i >= count) return;
     v4f sum = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < splits; ++s) sum += reinterpret_cast<const v4f *>(split_sums)[s * count + i];
-    const float top = *scale_top, back = 1.f / norms[i * 4 / n];
+    for (int s = 0; s < a.splits; ++s) sum += reinterpret_cast<const v4f *>(a.split_sums)[s * count + i];
+    const float top = *a.scale_top, back = 1.f / a.norms[i * 4 / a.n];
     uint32_t out[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) out[k] = to_16(sum[k] * top * back, bf16);
-    reinterpret_cast<u32x2 *>(dx)[i] = u32x2{out[0] | out[1] << 16, out[2] | out[3] << 16};
+    for (int k = 0; k < 4; ++k) out[k] = to_16(sum[k] * top * back, a.bf16);
+    reinterpret_cast<u32x2 *>(a.dx)[i] = u32x2{out[0] | out[1] << 16, out[2] | out[3] << 16};
 }
 
 template <typename S>
@@ -378,11 +386,6 @@ hipError_t go(SecondParams p, hipStream_t stream)
     const auto kernel = int8_second_kernel<S>;
     if (hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), S::BYTES)) return e;
     hipLaunchKernelGGL(kernel, dim3(p.column_tiles * p.token_tiles, (unsigned)p.splits), dim3(S::WAVES * 64), S::BYTES, stream, p);
-    if (hipError_t e = hipGetLastError()) return e;
-    if (p.splits == 1) return hipSuccess;
-    const int64_t threads = (int64_t)p.tokens * p.n / 4;
-    hipLaunchKernelGGL(int8_splits_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, p.split_sums, p.norms, p.scale_top, p.dx,
-                       (int64_t)p.tokens, p.n, p.splits, p.bf16);
     return hipGetLastError();
 }
 
@@ -422,37 +425,50 @@ hipError_t int8_backward_launch(const Int8Args &a, hipStream_t stream)
     const Int8Workspace ws = int8_workspace(a.matrices, a.m, a.n, a.tokens);
     unsigned char *base = static_cast<unsigned char *>(a.workspace);
     float *norms = reinterpret_cast<float *>(base + ws.norms), *scale_top = reinterpret_cast<float *>(base + ws.scale_top);
-    int64_t part_count = 0;
+    FinishParams f{};
+    f.parts = reinterpret_cast<const float *>(base + ws.parts);
+    f.split_sums = reinterpret_cast<const float *>(base + ws.split_sums);
+    f.norms = norms;
+    f.scale_top = scale_top;
+    f.dscales[0] = a.dscales[0];
+    f.dscales[1] = a.dscales[a.matrices - 1];
+    f.dx = a.dx;
+    f.m = a.m;
+    f.tokens = a.tokens;
+    f.n = (uint32_t)a.n;
+    f.sums_blocks = (uint32_t)((a.m * a.matrices + 63) / 64);
+    f.matrices = a.matrices;
+    f.splits = ws.splits;
+    f.bf16 = a.bf16;
     if (a.tokens > 0) {
         const bool whole = a.m % 8 == 0 && (reinterpret_cast<uintptr_t>(a.dy) & 15) == 0;
         hipLaunchKernelGGL(int8_norms_kernel, dim3((unsigned)(a.tokens + 1)), dim3(256), 0, stream, a.dy, a.channel_scales[0],
                            a.channel_scales[a.matrices - 1], norms, scale_top, a.m, a.bf16, whole);
         if (hipError_t e = hipGetLastError()) return e;
-        if (hipError_t e = int8_tile_backward_launch(a, ws, stream, part_count)) return e;
+        if (hipError_t e = int8_tile_backward_launch(a, ws, stream, f.part_count)) return e;
+        SecondParams p{};
+        p.grad = reinterpret_cast<const _Float16 *>(base + ws.grad);
+        p.w[0] = a.w[0];
+        p.w[1] = a.w[a.matrices - 1];
+        p.norms = norms;
+        p.scale_top = scale_top;
+        p.dx = a.dx;
+        p.m = (uint32_t)a.m;
+        p.m_padded = (uint32_t)(ws.grad_stride / a.matrices);
+        p.n = (uint32_t)a.n;
+        p.tokens = (uint32_t)a.tokens;
+        p.grad_stride = (uint32_t)ws.grad_stride;
+        p.matrices = a.matrices;
+        p.bf16 = a.bf16;
+        p.splits = ws.splits;
+        p.split_sums = reinterpret_cast<float *>(base + ws.split_sums);
+        // The large tile reads and converts a code for 128 tokens of a wave, the small one for 32, but a handful of tiles leaves most CUs idle.
+        const int64_t large = (int64_t)((p.n + 127) / 128) * ((p.tokens + 255) / 256) * p.splits;
+        if (hipError_t e = large >= 64 ? go<Large>(p, stream) : go<Small>(p, stream)) return e;
     }
-    hipLaunchKernelGGL(int8_sums_kernel, dim3((unsigned)((a.m * a.matrices + 63) / 64)), dim3(64), 0, stream,
-                       reinterpret_cast<const float *>(base + ws.parts), a.dscales[0], a.dscales[a.matrices - 1], a.m, a.matrices, part_count);
-    if (hipError_t e = hipGetLastError()) return e;
-    if (a.tokens == 0) return hipSuccess;
-    SecondParams p{};
-    p.grad = reinterpret_cast<const _Float16 *>(base + ws.grad);
-    p.w[0] = a.w[0];
-    p.w[1] = a.w[a.matrices - 1];
-    p.norms = norms;
-    p.scale_top = scale_top;
-    p.dx = a.dx;
-    p.m = (uint32_t)a.m;
-    p.m_padded = (uint32_t)(ws.grad_stride / a.matrices);
-    p.n = (uint32_t)a.n;
-    p.tokens = (uint32_t)a.tokens;
-    p.grad_stride = (uint32_t)ws.grad_stride;
-    p.matrices = a.matrices;
-    p.bf16 = a.bf16;
-    p.splits = ws.splits;
-    p.split_sums = reinterpret_cast<float *>(base + ws.split_sums);
-    // The large tile reads and converts a code for 128 tokens of a wave, the small one for 32, but a handful of tiles leaves most CUs idle.
-    const int64_t large = (int64_t)((p.n + 127) / 128) * ((p.tokens + 255) / 256) * p.splits;
-    return large >= 64 ? go<Large>(p, stream) : go<Small>(p, stream);
+    const int64_t split_blocks = ws.splits > 1 ? (a.tokens * a.n / 4 + 63) / 64 : 0;
+    hipLaunchKernelGGL(int8_finish_kernel, dim3((unsigned)(f.sums_blocks + split_blocks)), dim3(64), 0, stream, f);
+    return hipGetLastError();
 }
 
 }  // namespace bcq

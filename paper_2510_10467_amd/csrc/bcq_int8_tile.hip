@@ -460,9 +460,10 @@ void for_shapes(F f)
     // (the gated backward pass: a multiple of 64 channels, as the gradients' rows are)
     constexpr int ROW_WAVES = BACKWARD && MATS == 2 ? 2 : 1;
     f(TileShape<2, 4, 4, 2, 2>{}, 1.70f, 0.f);                                      // 256 x 256
-    f(TileShape<4, 2, 2, 2, 3>{}, 1.20f, 0.f);                                      // 256 x 128
+    f(TileShape<4, 2, 2, 2, 3>{}, 1.08f, 0.f);                                      // 256 x 128
     f(TileShape<2, 2, 2, 2, 2>{}, 0.72f, 1.12f);                                    // 128 x 128, two on a CU
     f(TileShape<2, 2, 2, 2, 4>{}, 0.60f, 0.f);                                      // 128 x 128
+    f(TileShape<2, 1, 2, 2, 6, 2, 64>{}, 0.34f, -1.f);                              // 128 x 64, two teams
     f(TileShape<ROW_WAVES, 2, 2, 1, ROW_WAVES == 2 ? 3 : 4>{}, ROW_WAVES * 0.37f, ROW_WAVES * 0.48f);          // 64 x 64 (128 x 64), two on a CU
     f(TileShape<ROW_WAVES, 2, 2, 1, ROW_WAVES == 2 ? 3 : 4, 2>{}, ROW_WAVES * 0.28f, 0.f);                     // 64 x 64 (128 x 64), two teams
 }
@@ -476,6 +477,10 @@ hipError_t pick(const TileParams &p, hipStream_t stream, int64_t *part_count = n
         using S = decltype(shape);
         const int64_t tiles = (int64_t)((p.m * MATS + S::ROWS - 1) / S::ROWS) * ((p.tokens + S::TOKS - 1) / S::TOKS);
         const int64_t each = (tiles + 255) / 256;                   // tiles of the busiest CU
+        if (beside < 0.f && each > 1) {                             // (ahead only where no CU has a second one)
+            ++index;
+            return;
+        }
         const float us = beside > 0.f ? (float)(each / 2) * beside + (float)(each % 2) * alone : (float)each * alone;
         if (chosen < 0 || us < best) {
             best = us;
