@@ -220,9 +220,9 @@ int bcq_quantize_form(const bcq_half *w, int p_low, int p_high, int cycles, int 
  *   w        int8 [m][n], channel_scales float [m]: output channel r's weights are channel_scales[r] * w[r][j]
  * bcq_int8_quantize makes both from 16-bit rows.  Any int8 value is a legal code.  16-bit tensors are binary16 or bfloat16 (`type`).
  *
- * Shape rules: 1 <= m <= 2^24 (backward passes: 2^20), 16 <= n <= 131056, n % 16 == 0 (a sum of n products of two codes fits 32 bits), 0 <= tokens <= 2^24,
- * m * tokens <= 2^40.  q, w, x and dx must be 16-byte aligned, y, h, dy and dh 2-byte, scales 4-byte.  No tokens: the forward calls do nothing (their per-token pointers
- * may be NULL), the backward calls write zeros to the scales' gradients.
+ * Shape rules: 1 <= m <= 2^24 (backward passes: 2^20), 16 <= n <= 131056, n % 16 == 0 (a sum of n products of two codes fits 32 bits),
+ * 0 <= tokens <= 2^23, m * tokens <= 2^37, n * tokens <= 2^37.  q, w, x and dx must be 16-byte aligned, y, h, dy and dh 2-byte, scales 4-byte.
+ * No tokens: the forward calls do nothing (their per-token pointers may be NULL), the backward calls write zeros to the scales' gradients.
  * Sums over columns are exact (32-bit integers), everything behind them is fp32, and results are rounded once to 16 bits.  Results do not depend
  * on what else is in the call's batch.
  */
@@ -238,6 +238,7 @@ typedef enum {
  * codes 0, so that what is computed from it is NaN and no other row is touched.
  *   x       [rows][n] of `type`
  *   q       int8 [rows][n] (written), scales float [rows] (written)
+ *   rows    0 <= rows <= 2^24 (0: no-op, the pointers may be NULL)
  * Activations: a row per token, at run time.  Weights: a row per output channel, offline.
  */
 int bcq_int8_quantize(const void *x, int type, int8_t *q, float *scales, int64_t rows, int64_t n, void *stream);

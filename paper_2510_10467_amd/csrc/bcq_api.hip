@@ -152,15 +152,16 @@ int run(const bcq::GemmArgs &a, hipStream_t stream)
     return err == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;
 }
 
-// 8-bit operators.  Row counts that keep tile numbers and byte offsets inside a tile in 32 bits.
-constexpr int64_t kInt8MaxRows = int64_t(1) << 24, kInt8MaxBackwardRows = int64_t(1) << 20;
+// 8-bit operators.  Sizes that keep the threads of a launch, tile numbers and byte offsets inside a tile in 32 bits.
+constexpr int64_t kInt8MaxRows = int64_t(1) << 24, kInt8MaxBackwardRows = int64_t(1) << 20, kInt8MaxTokens = int64_t(1) << 23;
 
 int check_int8(int type, int activation, int64_t m, int64_t n, int64_t tokens, int64_t max_m)
 {
     if (type != BCQ_FLOAT16 && type != BCQ_BFLOAT16) return BCQ_ERR_BAD_TYPE;
     if (activation != BCQ_ACT_SILU && activation != BCQ_ACT_GELU) return BCQ_ERR_BAD_TYPE;
     // 128 * 128 * n stays below 2^31
-    if (m < 1 || m > max_m || n < 16 || n > 131056 || n % 16 != 0 || tokens < 0 || tokens > kInt8MaxRows || m * tokens > int64_t(1) << 40)
+    if (m < 1 || m > max_m || n < 16 || n > 131056 || n % 16 != 0 || tokens < 0 || tokens > kInt8MaxTokens ||
+        m * tokens > int64_t(1) << 37 || n * tokens > int64_t(1) << 37)
         return BCQ_ERR_BAD_SHAPE;
     return BCQ_OK;
 }
@@ -479,7 +480,7 @@ int bcq_quantize_form(const bcq_half *w, int p_low, int p_high, int cycles, int 
 
 int bcq_int8_quantize(const void *x, int type, int8_t *q, float *scales, int64_t rows, int64_t n, void *stream)
 {
-    if (int rc = check_int8(type, BCQ_ACT_SILU, 1, n, rows, kInt8MaxRows)) return rc;
+    if (int rc = check_int8(type, BCQ_ACT_SILU, rows < 1 ? 1 : rows, n, rows < 0 ? -1 : 0, kInt8MaxRows)) return rc;
     if (rows == 0) return BCQ_OK;
     if (!x || !q || !scales) return BCQ_ERR_NULL;
     if (!aligned(x, 16) || !aligned(q, 16) || !aligned(scales, 4)) return BCQ_ERR_ALIGN;

@@ -315,7 +315,7 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_second_kernel(const Sec
 #pragma unroll
     for (int t = 0; t < (team == 0 ? S::FT : 0); ++t) {
         const uint32_t tok = (wt * S::FT + t) * 32 + r32;
-        const float back = 1.f / a.norms[t0 + min(tok, toks - 1)];      // (a power of two)
+        const float back = top / a.norms[t0 + min(tok, toks - 1)];      // (powers of two)
 #pragma unroll
         for (int c = 0; c < S::FC; ++c)
 #pragma unroll
@@ -323,7 +323,7 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_second_kernel(const Sec
                 const int col = (wc * S::FC + c) * 32 + 8 * e + 4 * half;
                 uint32_t out[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) out[i] = to_16(acc[c][t][4 * e + i] * top * back, a.bf16);
+                for (int i = 0; i < 4; ++i) out[i] = to_16(acc[c][t][4 * e + i] * back, a.bf16);
                 *reinterpret_cast<u32x2 *>(lds + tok * S::OUT_ROW + col * 2) = u32x2{out[0] | out[1] << 16, out[2] | out[3] << 16};
             }
     }
@@ -371,10 +371,10 @@ __global__ __launch_bounds__(64) void int8_finish_kernel(const FinishParams a)
     if (i >= count) return;
     v4f sum = {0.f, 0.f, 0.f, 0.f};
     for (int s = 0; s < a.splits; ++s) sum += reinterpret_cast<const v4f *>(a.split_sums)[s * count + i];
-    const float top = *a.scale_top, back = 1.f / a.norms[i * 4 / a.n];
+    const float back = *a.scale_top / a.norms[i * 4 / a.n];             // (powers of two)
     uint32_t out[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) out[k] = to_16(sum[k] * top * back, a.bf16);
+    for (int k = 0; k < 4; ++k) out[k] = to_16(sum[k] * back, a.bf16);
     reinterpret_cast<u32x2 *>(a.dx)[i] = u32x2{out[0] | out[1] << 16, out[2] | out[3] << 16};
 }
 

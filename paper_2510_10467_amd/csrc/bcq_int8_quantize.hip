@@ -78,11 +78,15 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void int8_codes_kern
 template <int THREADS, int CHUNKS>
 hipError_t go(const uint16_t *x, bool bf16, int8_t *q, float *scales, int64_t rows, int64_t n, hipStream_t stream)
 {
-    const int64_t blocks = THREADS == 64 ? (rows + 3) / 4 : rows;
-    const dim3 grid((unsigned)blocks), block(THREADS == 64 ? 256 : THREADS);
-    if (bf16) hipLaunchKernelGGL((int8_codes_kernel<THREADS, CHUNKS, true>), grid, block, 0, stream, x, q, scales, rows, (int)n);
-    else hipLaunchKernelGGL((int8_codes_kernel<THREADS, CHUNKS, false>), grid, block, 0, stream, x, q, scales, rows, (int)n);
-    return hipGetLastError();
+    constexpr int64_t MOST = int64_t(1) << 20;              // rows of a launch, whose threads are counted in 32 bits
+    for (int64_t r = 0; r < rows; r += MOST) {
+        const int64_t some = rows - r < MOST ? rows - r : MOST, blocks = THREADS == 64 ? (some + 3) / 4 : some;
+        const dim3 grid((unsigned)blocks), block(THREADS == 64 ? 256 : THREADS);
+        const auto kernel = bf16 ? int8_codes_kernel<THREADS, CHUNKS, true> : int8_codes_kernel<THREADS, CHUNKS, false>;
+        hipLaunchKernelGGL(kernel, grid, block, 0, stream, x + r * n, q + r * n, scales + r, some, (int)n);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace

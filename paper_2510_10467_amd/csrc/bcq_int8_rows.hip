@@ -185,11 +185,16 @@ hipError_t go(const RowsParams &p, hipStream_t stream)
 template <int MATS>
 hipError_t pick(const RowsParams &p, hipStream_t stream)
 {
+    // More tokens' codes are worth two blocks of rows, where those still give every CU a workgroup: 14336 x 4096 with 32 tokens 13.6 -> 11.3 us,
+    // with 64 tokens 21.4 -> 16.2 (4096 x 14336 the other way, 11.4 and 16.1 against 15.7 and 18.5); 35840 x 5120 with 16 tokens 41.4 -> 36.6
+    // (with 8 tokens 34.0 both, gated 17920 x 5120 with 16 tokens the other way, 37.6 against 41.5).
     const bool tall = p.m * MATS >= 8192;
     if (p.tokens <= 8) return go<0, MATS, 1, 4, 3>(p, stream);
-    if (p.tokens <= 16) return go<1, MATS, 1, 4, 3>(p, stream);
-    // More tokens' codes are worth two blocks of rows, where those still give every CU a workgroup: 14336 x 4096 with 32 tokens 13.6 -> 11.3 us,
-    // with 64 tokens 21.4 -> 16.2; 4096 x 14336 the other way, 11.4 and 16.1 against 15.7 and 18.5.
+    if (p.tokens <= 16) {
+        if constexpr (MATS == 1)
+            if (p.m >= 16384) return go<1, 1, 2, 4, 3>(p, stream);
+        return go<1, MATS, 1, 4, 3>(p, stream);
+    }
     if (p.tokens <= 32) return tall ? go<2, MATS, 2, 4, 2>(p, stream) : go<2, MATS, 1, 4, 3>(p, stream);
     if constexpr (MATS == 1)
         if (tall) return go<4, 1, 2, 4, 3>(p, stream);

@@ -6,13 +6,17 @@
 //              dc_r = sum_t dg s_t (sum_j q w)
 //
 // v_mfma_i32_32x32x32_i8, weights as rows and tokens as columns, so that a lane holds four neighbouring channels of one token.  A
-// workgroup's tile is ROWS weight rows by TOKS tokens; a step of 128 columns of both (8 and 8 KiB per 64 rows) goes from memory
-// into LDS by loads that write there, into one of two buffers while the other is multiplied.  The eight 16-byte parts of an LDS row sit
-// XOR-permuted by half the row's number, so that sixteen rows' operand reads use all banks.  A gated tile holds as many rows of gate as of up, by
-// turns of half a wave's rows.  Results go through LDS, to be stored in whole rows.
+// workgroup's tile is ROWS weight rows by TOKS tokens; a step of 64 or 128 columns of both goes from memory into LDS by loads that write there, into a
+// ring of steps.  The 16-byte parts of an LDS row sit XOR-permuted by the row's number, so that sixteen rows' operand reads use all banks.  A
+// gated tile holds as many rows of gate as of up, by turns of half a wave's rows.  Results go through LDS, to be stored in whole rows.
 //
 // Neighbouring workgroups' numbers go to different XCDs, each with a cache of its own: they are renumbered so that one XCD works on
 // the token tiles of the same weights.
+//
+// What bounds it: with every CU at work on large tiles the clock that the matrix pipe's power leaves (28672 x 8192 with 2048 tokens 461 us = 2090 TOP/s,
+// with codes of zero 415; the library's own 8-bit product of 8192^3 2100).  With few tiles the latency of a step, about 0.3 us where three
+// steps of 64 x 64 are under way.  Tall matrices with 33 to 128 tokens: the tiles of the last round, and the
+// weights' half of the bytes under way (17920 x 5120 gated with 48 tokens 52 us = 3.5 TB/s, with one token 33).
 #include <type_traits>
 
 #include "bcq_int8.hpp"
@@ -451,21 +455,19 @@ hipError_t go(TileParams p, hipStream_t stream, int64_t *part_count)
     return hipGetLastError();
 }
 
-// What a workgroup takes per 128 columns where the chip is full, alone on its CU and, where two fit, beside a second one (microseconds, measured):
-// the shape that is expected to be done first is taken.  Large tiles read each operand from the caches the fewest times; small ones, with teams or a
-// deep ring, give every CU work and keep enough bytes under way where there are few.
+// What a workgroup takes per 128 columns, alone on its CU and as one of several in turn (microseconds, measured): the shape that is expected to be done
+// first is taken.  Large tiles read each operand from the caches the fewest times; small ones, with teams or a deep ring, give every CU work and
+// keep enough bytes under way where there are few.  (4096 columns: 4096 rows and 256 tokens 52 / 31 / 20 / 16 / 11 us from the first shape to the last,
+// 14336 rows and 2048 tokens, gated, 248 / 261 / 314 / 512 / 630.)
 template <int MATS, bool BACKWARD, typename F>
 void for_shapes(F f)
 {
-    // (the gated backward pass: a multiple of 64 channels, as the gradients' rows are)
-    constexpr int ROW_WAVES = BACKWARD && MATS == 2 ? 2 : 1;
-    f(TileShape<2, 4, 4, 2, 2>{}, 1.70f, 0.f);                                      // 256 x 256
-    f(TileShape<4, 2, 2, 2, 3>{}, 1.08f, 0.f);                                      // 256 x 128
-    f(TileShape<2, 2, 2, 2, 2>{}, 0.72f, 1.12f);                                    // 128 x 128, two on a CU
-    f(TileShape<2, 2, 2, 2, 4>{}, 0.60f, 0.f);                                      // 128 x 128
-    f(TileShape<2, 1, 2, 2, 6, 2, 64>{}, 0.34f, -1.f);                              // 128 x 64, two teams
-    f(TileShape<ROW_WAVES, 2, 2, 1, ROW_WAVES == 2 ? 3 : 4>{}, ROW_WAVES * 0.37f, ROW_WAVES * 0.48f);          // 64 x 64 (128 x 64), two on a CU
-    f(TileShape<ROW_WAVES, 2, 2, 1, ROW_WAVES == 2 ? 3 : 4, 2>{}, ROW_WAVES * 0.28f, 0.f);                     // 64 x 64 (128 x 64), two teams
+    f(TileShape<2, 4, 4, 2, 2>{}, 1.70f, 1.70f);            // 256 x 256
+    f(TileShape<4, 2, 2, 2, 3>{}, 1.08f, 1.10f);            // 256 x 128
+    f(TileShape<2, 2, 2, 2, 4>{}, 0.60f, 0.62f);            // 128 x 128
+    f(TileShape<2, 1, 2, 2, 6, 2, 64>{}, 0.34f, 0.50f);     // 128 x 64, two teams
+    // 64 x 64, two teams (a tile of the gated backward pass has a multiple of 64 channels, as the gradients' rows have)
+    if constexpr (!BACKWARD || MATS == 1) f(TileShape<1, 2, 2, 1, 4, 2>{}, 0.28f, 0.30f);
 }
 
 template <int MATS, bool BACKWARD>
@@ -473,15 +475,11 @@ hipError_t pick(const TileParams &p, hipStream_t stream, int64_t *part_count = n
 {
     float best = 0.f;
     int index = 0, chosen = -1;
-    for_shapes<MATS, BACKWARD>([&](auto shape, float alone, float beside) {
+    for_shapes<MATS, BACKWARD>([&](auto shape, float alone, float in_turn) {
         using S = decltype(shape);
         const int64_t tiles = (int64_t)((p.m * MATS + S::ROWS - 1) / S::ROWS) * ((p.tokens + S::TOKS - 1) / S::TOKS);
         const int64_t each = (tiles + 255) / 256;                   // tiles of the busiest CU
-        if (beside < 0.f && each > 1) {                             // (ahead only where no CU has a second one)
-            ++index;
-            return;
-        }
-        const float us = beside > 0.f ? (float)(each / 2) * beside + (float)(each % 2) * alone : (float)each * alone;
+        const float us = each == 1 ? alone : (float)each * in_turn;
         if (chosen < 0 || us < best) {
             best = us;
             chosen = index;

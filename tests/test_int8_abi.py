@@ -21,7 +21,7 @@ def changed(args, **by):
 
 # the shapes that every entry point refuses: (m, n, tokens)
 BAD_SHAPES = [(0, 64, 4), (-1, 64, 4), (8, 0, 4), (8, 8, 4), (8, 40, 4), (8, 131072, 4), (8, 131064, 4), (8, 64, -1), ((1 << 24) + 1, 64, 4),
-              (8, 64, (1 << 24) + 1), (1 << 20, 64, (1 << 20) + 1)]
+              (8, 64, (1 << 23) + 1), (1 << 20, 64, (1 << 17) + 1), (8, 131056, (1 << 20) + 256)]
 
 
 def test_quantize(lib):
@@ -83,7 +83,7 @@ def test_workspace(lib):
     assert size(1, 1000, 64, 100) >= 2 * 1000 * 100
     assert size(2, 1000, 64, 100) >= 2 * 2 * 1000 * 100
     assert size(2, 14336, 64, 4096) > size(1, 14336, 64, 4096) > size(1, 14336, 64, 4095)
-    assert size(2, 1 << 20, 64, 1 << 20) > 1 << 42
+    assert size(2, 1 << 20, 64, 1 << 17) > 1 << 39
 
 
 def test_gemm_backward(lib):
