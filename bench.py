@@ -50,7 +50,7 @@ def parse_args():
     ap.add_argument("--details", action="store_true", help="also time every (layer, p) kernel and an fp16 GEMV")
     ap.add_argument("--calibrate-copy", action="store_true",
                     help="also run a plain 256 MiB device copy a few times (a reference kernel of known traffic for counter runs)")
-    ap.add_argument("--suite", choices=["decode", "mixed", "large", "phi4", "fused", "offset", "quant", "step", "issue", "generic"], default=None,
+    ap.add_argument("--suite", choices=["decode", "mixed", "large", "phi4", "fused", "offset", "quant", "step", "issue", "generic", "int8"], default=None,
                     help="instead of the headline workload, time another workload family and print its table")
     return ap.parse_args()
 
@@ -259,6 +259,34 @@ def run_suite(args, torch, bcq, syn, dev):
                              "ms_per_token": round(ms / batch, 4), "GBps": round(by / ms / 1e6, 1),
                              "pct_of_hbm_peak": round(100 * by / ms / 1e6 / HBM_PEAK_GBS, 2),
                              "tokens_per_s_upper_bound": round(batch * 1e3 / ms, 1)})
+    elif args.suite == "int8":
+        # The 8-bit operators on the same layers: the quantiser of tokens, the product, the gated block, and the gradients of both.  TOP/s
+        # counts two operations for each weight that a token meets in every product of a call, GB/s what it reads and writes at least.
+        def codes(rows, cols):
+            return (torch.randint(-127, 128, (rows, cols), dtype=torch.int8, device=dev, generator=gen),
+                    (0.5 + torch.rand(rows, device=dev, generator=gen)) * 1e-2)
+        for (m, n) in ((4096, 14336), (14336, 4096), (28672, 8192)):
+            copies = min(24, max(2, -(-MIN_ROTATION_BYTES // (2 * m * n))))
+            sets = [(*codes(m, n), *codes(m, n)) for _ in range(copies)]
+            for batch in (1, 16, 64, 256, 2048):
+                q, ts = codes(batch, n)
+                x, dy = (torch.randn((batch, width), device=dev, generator=gen).half() for width in (n, m))
+                calls = {"quantize": (lambda w, c, u, d: bcq.bcq_int8_quantize(x), 0, 3 * batch * n),
+                         "gemm": (lambda w, c, u, d: bcq.bcq_int8_gemm(q, ts, w, c), 1, m * n + batch * (n + 2 * m)),
+                         "gated": (lambda w, c, u, d: bcq.bcq_int8_gated(q, ts, w, c, u, d), 2, 2 * m * n + batch * (n + 2 * m))}
+                if batch >= 64:
+                    calls["gemm_backward"] = (lambda w, c, u, d: bcq.bcq_int8_gemm_backward(dy, q, ts, w, c), 2, m * n + batch * (3 * n + 2 * m))
+                    calls["gated_backward"] = (lambda w, c, u, d: bcq.bcq_int8_gated_backward(dy, q, ts, w, c, u, d), 4,
+                                               2 * m * n + batch * (3 * n + 2 * m))
+                for name, (call, products, by) in calls.items():
+                    def burst():
+                        for i in range(launches):
+                            call(*sets[i % copies])
+                    us = timed_graph(burst, reps=5) * 1e3 / launches
+                    rows.append({"operator": f"bcq_int8_{name}", "m": m, "n": n, "tokens": batch, "us": round(us, 2), "GBps": round(by / us / 1e3, 1),
+                                 "pct_of_hbm_peak": round(100 * by / us / 1e3 / HBM_PEAK_GBS, 2),
+                                 "TOPs": round(2.0 * products * m * n * batch / us / 1e6, 1)})
+            del sets
     elif args.suite == "issue":
         # What one SIMD issues when matrix and vector instructions alternate (include/bcq_bench.h): shader-clock ticks per
         # matrix instruction for one wave per SIMD (4 waves) and for two (8).  A matrix instruction keeps its SIMD from
