@@ -2,13 +2,17 @@
 //
 //   norms     per token the power of two f_t that brings its largest |dy| to [1/32, 1/16), and the power of two above all channel scales, S
 //   first     (bcq_int8_tile.hip) G = binary16 of f_t dg c / S for every channel of every matrix, and partial sums of dc
-//   sums      dc: the partial sums of a channel, in order
 //   second    dx = (S / f_t) sum over channels of G w: a product over the weights' ROWS
+//   finish    dc: the partial sums of a channel, in order; dx where the channels were taken in several runs: the runs' sums, in order
 //
 // The second product runs on v_mfma_f32_32x32x16_f16.  Both operands go into LDS by loads that write there, the weights as they are stored: 64
 // rows of 8-bit codes by a tile's columns.  A lane needs eight codes of one column, which is what the transposing LDS read of
 // 8-bit values delivers (16 lanes take eight rows of 16 columns), and turns them into binary16, exactly: a code's byte
 // with its sign bit turned under the byte 0x64 is the number 1024 + 128 + code.
+//
+// What bounds it: the power of the matrix pipe on random operands (2048 tokens, 4096 columns, 2 x 14336 channels: 450 us = 1070 TFLOP/s, with gradients of
+// zero 389; the library's plain binary16 product of 8192^3 reaches 1300) and the codes' conversion (without it 400).  The whole gated
+// backward pass of that size: 743 us, of which the norms 12, the first half 290, the finish 5.
 #include "bcq_int8.hpp"
 #include "bcq_internal.hpp"
 
@@ -390,7 +394,9 @@ hipError_t go(SecondParams p, hipStream_t stream)
 }
 
 using Large = SecondShape<2, 2, 2, 4, 2, 2>;            // 128 columns x 256 tokens, two teams
-using Small = SecondShape<2, 2, 1, 1, 4, 2>;            // 64 x 64, two teams
+using Middle = SecondShape<2, 2, 2, 2, 3, 2>;           // 128 x 128
+using Narrow = SecondShape<4, 1, 1, 2, 3, 2>;           // 128 x 64
+using Small = SecondShape<2, 2, 1, 1, 4, 2>;            // 64 x 64
 
 // Few columns and tokens, many channels: the channels in up to eight runs, of 8 steps at least, as long as every CU gets one workgroup (4096 columns,
 // 512 tokens, 2 x 14336 channels: 300 us in one run, 70 in four).
@@ -462,9 +468,15 @@ hipError_t int8_backward_launch(const Int8Args &a, hipStream_t stream)
         p.bf16 = a.bf16;
         p.splits = ws.splits;
         p.split_sums = reinterpret_cast<float *>(base + ws.split_sums);
-        // The large tile reads and converts a code for 128 tokens of a wave, the small one for 32, but a handful of tiles leaves most CUs idle.
-        const int64_t large = (int64_t)((p.n + 127) / 128) * ((p.tokens + 255) / 256) * p.splits;
-        if (hipError_t e = large >= 64 ? go<Large>(p, stream) : go<Small>(p, stream)) return e;
+        // A wave of the large tile converts a code for 128 tokens.  Up to 128 or 64 tokens a tile of as many wastes no matrix instructions (gemm,
+        // 14336 x 4096 with 64 tokens 58 -> 48 us in all, with 128 tokens 68 -> 63); where a handful of tiles leaves most CUs idle the
+        // small one is ahead (1000 x 1024 with 100 tokens 20 -> 18).
+        const int64_t workgroups = (int64_t)((p.n + 127) / 128) * ((p.tokens + 255) / 256) * p.splits;
+        if (hipError_t e = workgroups < 64      ? go<Small>(p, stream)
+                           : p.tokens <= 64     ? go<Narrow>(p, stream)
+                           : p.tokens <= 128    ? go<Middle>(p, stream)
+                                                : go<Large>(p, stream))
+            return e;
     }
     const int64_t split_blocks = ws.splits > 1 ? (a.tokens * a.n / 4 + 63) / 64 : 0;
     hipLaunchKernelGGL(int8_finish_kernel, dim3((unsigned)(f.sums_blocks + split_blocks)), dim3(64), 0, stream, f);
