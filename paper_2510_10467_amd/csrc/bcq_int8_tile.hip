@@ -16,7 +16,7 @@
 // What bounds it: with every CU at work on large tiles the clock that the matrix pipe's power leaves (28672 x 8192 with 2048 tokens 461 us = 2090 TOP/s,
 // with codes of zero 415; the library's own 8-bit product of 8192^3 2100).  With few tiles the latency of a step, about 0.3 us where three
 // steps of 64 x 64 are under way.  Tall matrices with 33 to 128 tokens: the tiles of the last round, and the
-// weights' half of the bytes under way (17920 x 5120 gated with 48 tokens 52 us = 3.5 TB/s, with one token 33).
+// weights' half of the bytes under way (17920 x 5120 gated with 48 tokens 47 us = 3.9 TB/s, with one token 33).
 #include <type_traits>
 
 #include "bcq_int8.hpp"
@@ -457,14 +457,15 @@ hipError_t go(TileParams p, hipStream_t stream, int64_t *part_count)
 
 // What a workgroup takes per 128 columns, alone on its CU and as one of several in turn (microseconds, measured): the shape that is expected to be done
 // first is taken.  Large tiles read each operand from the caches the fewest times; small ones, with teams or a deep ring, give every CU work and
-// keep enough bytes under way where there are few.  (4096 columns: 4096 rows and 256 tokens 52 / 31 / 20 / 16 / 11 us from the first shape to the last,
-// 14336 rows and 2048 tokens, gated, 248 / 261 / 314 / 512 / 630.)
+// keep enough bytes under way where there are few.  (4096 columns: 4096 rows and 256 tokens 52 / 31 / 20 / 22 / 15 / 11 us from the first shape to the last,
+// 14336 rows and 512 tokens, gated, 65 / 75 / 90 / 106 / 131 / 162.  5120 columns, 17920 rows and 48 tokens, gated: 78 / 56 / 62 / 47 / 65 / 52.)
 template <int MATS, bool BACKWARD, typename F>
 void for_shapes(F f)
 {
     f(TileShape<2, 4, 4, 2, 2>{}, 1.70f, 1.70f);            // 256 x 256
     f(TileShape<4, 2, 2, 2, 3>{}, 1.08f, 1.10f);            // 256 x 128
     f(TileShape<2, 2, 2, 2, 4>{}, 0.60f, 0.62f);            // 128 x 128
+    f(TileShape<4, 1, 2, 2, 4>{}, 0.69f, 0.70f);            // 256 x 64
     f(TileShape<2, 1, 2, 2, 6, 2, 64>{}, 0.34f, 0.50f);     // 128 x 64, two teams
     // 64 x 64, two teams (a tile of the gated backward pass has a multiple of 64 channels, as the gradients' rows have)
     if constexpr (!BACKWARD || MATS == 1) f(TileShape<1, 2, 2, 1, 4, 2>{}, 0.28f, 0.30f);
