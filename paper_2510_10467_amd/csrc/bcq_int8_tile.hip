@@ -253,7 +253,9 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_tile_kernel(const TileP
     int buffer = 0, into = AHEAD, i = 0;
     auto next = [](int b) { return b + 1 == S::RING ? 0 : b + 1; };
     for (; i + AHEAD < rounds; ++i) {                       // (whole steps: the last one is still to come)
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD - (S::ACROSS ? 2 : 1)) * LOADS) : "memory");
+        constexpr int UNDER_WAY = (AHEAD - (S::ACROSS ? 2 : 1)) * LOADS;
+        if constexpr (S::TEAM_WAVES == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(UNDER_WAY) : "memory");     // (a ring of its own)
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(UNDER_WAY) : "memory");
         if (S::TEAMS == 1 || step(i + AHEAD) < stages) stage(into, (uint32_t)step(i + AHEAD) * S::STEP);
         whole_step(buffer, next(buffer));
         buffer = next(buffer);
@@ -457,8 +459,9 @@ hipError_t go(TileParams p, hipStream_t stream, int64_t *part_count)
 
 // What a workgroup takes per 128 columns, alone on its CU and as one of several in turn (microseconds, measured): the shape that is expected to be done
 // first is taken.  Large tiles read each operand from the caches the fewest times; small ones, with teams or a deep ring, give every CU work and
-// keep enough bytes under way where there are few.  (4096 columns: 4096 rows and 256 tokens 52 / 31 / 20 / 22 / 15 / 11 us from the first shape to the last,
-// 14336 rows and 512 tokens, gated, 65 / 75 / 90 / 106 / 131 / 162.  5120 columns, 17920 rows and 48 tokens, gated: 78 / 56 / 62 / 47 / 65 / 52.)
+// keep enough bytes under way where there are few.  (4096 columns: 4096 rows and 256 tokens 52 / 31 / 20 / 22 / 15 / 11 / 15 us from the first shape to the last,
+// 14336 rows and 512 tokens, gated, 65 / 75 / 90 / 106 / 131 / 162.  5120 columns, 17920 rows and 48 tokens, gated: 78 / 56 / 62 / 47 / 65 / 52.  4096 x 4096 with 100 tokens:
+// the last two 10.4 and 8.1.)
 template <int MATS, bool BACKWARD, typename F>
 void for_shapes(F f)
 {
@@ -467,8 +470,10 @@ void for_shapes(F f)
     f(TileShape<2, 2, 2, 2, 4>{}, 0.60f, 0.62f);            // 128 x 128
     f(TileShape<4, 1, 2, 2, 4>{}, 0.69f, 0.70f);            // 256 x 64
     f(TileShape<2, 1, 2, 2, 6, 2, 64>{}, 0.34f, 0.50f);     // 128 x 64, two teams
-    // 64 x 64, two teams (a tile of the gated backward pass has a multiple of 64 channels, as the gradients' rows have)
-    if constexpr (!BACKWARD || MATS == 1) f(TileShape<1, 2, 2, 1, 4, 2>{}, 0.28f, 0.30f);
+    if constexpr (!BACKWARD || MATS == 1) {                 // (a tile of the gated backward pass has 64 channels or more, as the gradients' rows have)
+        f(TileShape<1, 2, 2, 1, 4, 2>{}, 0.28f, 0.30f);     // 64 x 64, two teams
+        f(TileShape<1, 1, 2, 1, 3, 4>{}, 0.20f, 0.20f);     // 64 x 32, four teams
+    }
 }
 
 template <int MATS, bool BACKWARD>
