@@ -79,6 +79,7 @@ hipError_t int8_tile_launch(const Int8Args &a, hipStream_t stream);
 struct Int8Workspace {
     int64_t grad_stride;            // halves between tokens: matrices * m rounded up to 64
     int splits;                     // runs of channels whose contributions to dx are summed apart
+    int second_shape;               // ... and the tiles that they are taken in
     int64_t grad, norms, scale_top, parts, split_sums, bytes;       // offsets in bytes, and the whole
     int64_t part_count;             // room for so many partial sums of a channel
 };

@@ -374,6 +374,7 @@ __global__ __launch_bounds__(64) void int8_finish_kernel(const FinishParams a)
     const int64_t i = (int64_t)(blockIdx.x - a.sums_blocks) * 64 + threadIdx.x, count = a.tokens * a.n / 4;
     if (i >= count) return;
     v4f sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int s = 0; s < a.splits; ++s) sum += reinterpret_cast<const v4f *>(a.split_sums)[s * count + i];
     const float back = *a.scale_top / a.norms[i * 4 / a.n];             // (powers of two)
     uint32_t out[4];
@@ -393,19 +394,46 @@ hipError_t go(SecondParams p, hipStream_t stream)
     return hipGetLastError();
 }
 
-using Large = SecondShape<2, 2, 2, 4, 2, 2>;            // 128 columns x 256 tokens, two teams
-using Middle = SecondShape<2, 2, 2, 2, 3, 2>;           // 128 x 128
-using Narrow = SecondShape<4, 1, 1, 2, 3, 2>;           // 128 x 64
-using Small = SecondShape<2, 2, 1, 1, 4, 2>;            // 64 x 64
-
-// Few columns and tokens, many channels: the channels in up to eight runs, of 8 steps at least, as long as every CU gets one workgroup (4096 columns,
-// 512 tokens, 2 x 14336 channels: 300 us in one run, 70 in four).
-int second_splits(int matrices, int64_t m, int64_t n, int64_t tokens)
+// What a workgroup takes per step of 64 channels, alone on its CU and as one of two or more, each (microseconds, measured: gemm, 14336 x 4096 with 32 to
+// 128 tokens, 4096 x 14336 with 512).  A wave turns a code into binary16 for all of its tile's tokens: with 32 columns of it in a wave instead of 64, twice, the
+// second half of 4096 x 14336 with 512 tokens went from 70 to 65 us.
+template <typename F>
+void for_shapes(F f)
 {
-    const int64_t tiles = ((n + 127) / 128) * ((tokens + 255) / 256), steps = matrices * ((m + 63) / 64);
-    int splits = 1;
-    while (splits < 8 && tiles * splits * 2 <= 256 && steps >= 8 * splits * 2) splits *= 2;
-    return splits;
+    f(SecondShape<8, 1, 1, 4, 2, 2>{}, 0.85f, 1.02f);       // 256 columns x 128 tokens, two teams
+    f(SecondShape<4, 1, 1, 4, 3>{}, 0.50f, 0.56f);          // 128 x 128: two share a CU
+    f(SecondShape<4, 1, 1, 2, 2, 2>{}, 0.50f, 0.40f);       // 128 x 64, two teams: two share a CU
+    f(SecondShape<2, 2, 1, 1, 4, 2>{}, 0.40f, 0.40f);       // 64 x 64, two teams
+}
+
+// The shape, and in how many runs the channels are taken where few columns and tokens leave CUs without work: what is expected to be done first, with
+// four steps for a workgroup's start and end, and the runs' sums, written and read, at 8 TB/s.  (4096 columns, 48 tokens, 2 x 14336 channels, the
+// whole pass: 161 us in two runs, 101 in four, 74 in eight, 70 in 16.)
+struct SecondPlan {
+    int shape, splits;
+};
+SecondPlan second_plan(int matrices, int64_t m, int64_t n, int64_t tokens)
+{
+    const int64_t steps = matrices * ((m + 63) / 64);
+    SecondPlan plan{0, 1};
+    float best = 0.f;
+    int index = 0;
+    for_shapes([&](auto shape, float alone, float shared) {
+        using S = decltype(shape);
+        const int64_t tiles = ((n + S::COLS - 1) / S::COLS) * ((tokens + S::TOKS - 1) / S::TOKS);
+        for (int splits = 1; splits <= 16; ++splits) {
+            const int64_t run = (steps + splits - 1) / splits, each = (tiles * splits + 255) / 256;
+            if (splits > 1 && run < 4) break;
+            const float us = (float)(run + 4) * (each <= 1 ? alone : (float)each * shared) +
+                             (splits > 1 ? 1.f + (float)splits * (float)tokens * (float)n * (8.f / 8e6f) : 0.f);
+            if (best == 0.f || us < best) {
+                best = us;
+                plan = {index, splits};
+            }
+        }
+        ++index;
+    });
+    return plan;
 }
 
 }  // namespace
@@ -415,8 +443,10 @@ Int8Workspace int8_workspace(int matrices, int64_t m, int64_t n, int64_t tokens)
     Int8Workspace ws;
     auto up = [](int64_t bytes) { return (bytes + 255) / 256 * 256; };
     ws.grad_stride = matrices * ((m + 63) / 64 * 64);
-    ws.part_count = (tokens + 63) / 64 * 2 + 2;             // at most: a wave's tokens are 64, or 32 in tiles of 64
-    ws.splits = second_splits(matrices, m, n, tokens);
+    ws.part_count = (tokens + 63) / 64 * 2 + 2;             // at most: a wave's tokens are 64, or 32 in tiles of 64 and 32
+    const SecondPlan plan = second_plan(matrices, m, n, tokens);
+    ws.second_shape = plan.shape;
+    ws.splits = plan.splits;
     ws.grad = 0;
     ws.norms = up(tokens * ws.grad_stride * 2);
     ws.scale_top = ws.norms + up(tokens * 4);
@@ -468,15 +498,12 @@ hipError_t int8_backward_launch(const Int8Args &a, hipStream_t stream)
         p.bf16 = a.bf16;
         p.splits = ws.splits;
         p.split_sums = reinterpret_cast<float *>(base + ws.split_sums);
-        // A wave of the large tile converts a code for 128 tokens.  Up to 128 or 64 tokens a tile of as many wastes no matrix instructions (gemm,
-        // 14336 x 4096 with 64 tokens 58 -> 48 us in all, with 128 tokens 68 -> 63); where a handful of tiles leaves most CUs idle the
-        // small one is ahead (1000 x 1024 with 100 tokens 20 -> 18).
-        const int64_t workgroups = (int64_t)((p.n + 127) / 128) * ((p.tokens + 255) / 256) * p.splits;
-        if (hipError_t e = workgroups < 64      ? go<Small>(p, stream)
-                           : p.tokens <= 64     ? go<Narrow>(p, stream)
-                           : p.tokens <= 128    ? go<Middle>(p, stream)
-                                                : go<Large>(p, stream))
-            return e;
+        hipError_t result = hipErrorInvalidValue;
+        int index = 0;
+        for_shapes([&](auto shape, float, float) {
+            if (index++ == ws.second_shape) result = go<decltype(shape)>(p, stream);
+        });
+        if (result) return result;
     }
     const int64_t split_blocks = ws.splits > 1 ? (a.tokens * a.n / 4 + 63) / 64 : 0;
     hipLaunchKernelGGL(int8_finish_kernel, dim3((unsigned)(f.sums_blocks + split_blocks)), dim3(64), 0, stream, f);

@@ -273,6 +273,9 @@ def test_no_tokens(bcq):
 
 BACKWARD_SIZES = [(1, 1, 16), (2, 40, 48), (16, 17, 64), (33, 64, 128), (64, 65, 144), (77, 101, 1040), (130, 129, 80), (300, 200, 2064), (65, 1000, 272),
                   (513, 63, 16)]
+# each tile of the second product, with the channels in one run and in several
+SECOND_SIZES = [(50, 3003, 20000), (300, 1001, 14352), (300, 1001, 4112), (700, 900, 6160)]
+SECOND_GATED = [(40, 2000, 14352), (300, 2001, 6160), (129, 1500, 4112), (520, 1001, 14352)]
 
 
 def second_half_error(err, grads, cs, w, top, norm):
@@ -298,7 +301,7 @@ def sums_error(terms, err, tokens):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("tokens, m, n", BACKWARD_SIZES + LARGE_SIZES[3:5] + LARGE_SIZES[7:] + [(300, 33001, 80), (300, 72, 33040), (100, 2000, 2000)])
+@pytest.mark.parametrize("tokens, m, n", BACKWARD_SIZES + LARGE_SIZES[3:5] + LARGE_SIZES[7:] + SECOND_SIZES + [(300, 33001, 80), (300, 72, 33040), (100, 2000, 2000)])
 def test_gemm_backward(bcq, dtype, tokens, m, n):
     gen = generator("gemm_backward", tokens, m, n)
     q, ts, [(w, cs)] = operands(tokens, m, n, gen)
@@ -317,7 +320,7 @@ def test_gemm_backward(bcq, dtype, tokens, m, n):
 
 @pytest.mark.parametrize("activation", ["silu", "gelu"])
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("tokens, m, n", BACKWARD_SIZES + LARGE_GATED[2:] + [(300, 16421, 80), (300, 72, 33040), (100, 1000, 2000)])
+@pytest.mark.parametrize("tokens, m, n", BACKWARD_SIZES + LARGE_GATED[2:] + SECOND_GATED + [(300, 16421, 80), (300, 72, 33040), (100, 1000, 2000)])
 def test_gated_backward(bcq, dtype, activation, tokens, m, n):
     gen = generator("gated_backward", tokens, m, n)
     q, ts, [(wg, cg), (wu, cu)] = operands(tokens, m, n, gen, 2)
