@@ -275,35 +275,38 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_tile_kernel(const TileP
             multiply(o);
         }
     __syncthreads();
-    // the other teams' sums to the first
-    if constexpr (S::TEAMS > 1) {
+    // The teams add up: of each tile's four groups of four channels a team ends with GROUPS, its own sums and what the others left it.
+    constexpr int GROUPS = 4 / S::TEAMS;
+    v4i sums_of[S::FR][S::FT][GROUPS];
+#pragma unroll
+    for (int k = 0; k < S::TEAMS; ++k) {
+        if (team != k) continue;
         v4i *const exchange = reinterpret_cast<v4i *>(lds) + tw * (S::FR * S::FT * 4 * 64) + lane;
         constexpr int BETWEEN = S::TEAM_WAVES * S::FR * S::FT * 4 * 64;
-        if (team > 0) {
+#pragma unroll
+        for (int r = 0; r < S::FR; ++r)
+#pragma unroll
+            for (int t = 0; t < S::FT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const v4i v = {acc[r][t][4 * e], acc[r][t][4 * e + 1], acc[r][t][4 * e + 2], acc[r][t][4 * e + 3]};
+                    const int whose = e / GROUPS;                   // its place among those that leave something for that team: all but itself
+                    if (whose == k) sums_of[r][t][e % GROUPS] = v;
+                    else exchange[(k - (k > whose ? 1 : 0)) * BETWEEN + ((r * S::FT + t) * 4 + e) * 64] = v;
+                }
+    }
+    if constexpr (S::TEAMS > 1) {
+        __syncthreads();
+        const v4i *const exchange = reinterpret_cast<const v4i *>(lds) + tw * (S::FR * S::FT * 4 * 64) + team * GROUPS * 64 + lane;
+        constexpr int BETWEEN = S::TEAM_WAVES * S::FR * S::FT * 4 * 64;
+#pragma unroll
+        for (int k = 0; k < S::TEAMS - 1; ++k)
 #pragma unroll
             for (int r = 0; r < S::FR; ++r)
 #pragma unroll
                 for (int t = 0; t < S::FT; ++t)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        exchange[(team - 1) * BETWEEN + ((r * S::FT + t) * 4 + e) * 64] =
-                            v4i{acc[r][t][4 * e], acc[r][t][4 * e + 1], acc[r][t][4 * e + 2], acc[r][t][4 * e + 3]};
-        }
-        __syncthreads();
-        if (team == 0) {
-#pragma unroll
-            for (int k = 0; k < S::TEAMS - 1; ++k)
-#pragma unroll
-                for (int r = 0; r < S::FR; ++r)
-#pragma unroll
-                    for (int t = 0; t < S::FT; ++t)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const v4i v = exchange[k * BETWEEN + ((r * S::FT + t) * 4 + e) * 64];
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) acc[r][t][4 * e + c] += v[c];
-                        }
-        }
+                    for (int e = 0; e < GROUPS; ++e) sums_of[r][t][e] += exchange[k * BETWEEN + ((r * S::FT + t) * 4 + e) * 64];
         __syncthreads();
     }
 
@@ -363,8 +366,8 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_tile_kernel(const TileP
                     [[maybe_unused]] float norm = 0.f;
                     if constexpr (BACKWARD) norm = norms[tok];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int ch = (wr * FRC + r) * 32 + 8 * e + 4 * half;     // element 4 e + i: channel ch + i
+                    for (int e = 0; e < GROUPS; ++e) {
+                        const int ch = (wr * FRC + r) * 32 + 8 * (team * GROUPS + e) + 4 * half;    // element i: channel ch + i
                         unsigned char *at = lds + tok * L::OUT_ROW + ch * 2;
                         const v4f c0 = *reinterpret_cast<const v4f *>(scales + ch);
                         const v4f c1 = *reinterpret_cast<const v4f *>(scales + (MATS - 1) * CHANNELS + ch);
@@ -373,9 +376,9 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_tile_kernel(const TileP
                         uint32_t out[4], out2[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const float p = (float)acc[r][t][4 * e + i] * ts;
+                            const float p = (float)sums_of[r][t][e][i] * ts;
                             [[maybe_unused]] float p2 = 0.f, slope = 0.f;
-                            if constexpr (MATS == 2) p2 = (float)acc[FRC + r][t][4 * e + i] * ts;
+                            if constexpr (MATS == 2) p2 = (float)sums_of[FRC + r][t][e][i] * ts;
                             if constexpr (!BACKWARD) {
                                 float v = p * c0[i];
                                 if constexpr (MATS == 2) v = activate<false>(v, ACT, slope) * (p2 * c1[i]);
@@ -407,16 +410,16 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_tile_kernel(const TileP
                     }
                 }
             if constexpr (BACKWARD) {
-                // lane l of a half gets value l: element l % 16 of the first or second sixteen
+                // lane l of a half gets value l: element l % 16 of the first or second sixteen, of which the team has 4 GROUPS
                 const float sum = sums_of_32(sums, lane);
                 const int second = r32 >> 4, e = (r32 >> 2) & 3, i = r32 & 3;
-                const uint32_t ch = (wr * FRC + r0 + (MATS == 1 ? second : 0)) * 32 + 8 * e + 4 * half + i;
+                const uint32_t ch = (wr * FRC + r0 + (MATS == 1 ? second : 0)) * 32 + 8 * (team * GROUPS + e) + 4 * half + i;
                 float *parts = a.parts + (int64_t)(token_tile * S::WT + wt) * MATS * a.m;
-                if (ch < chs) parts[(int64_t)(MATS == 1 ? 0 : second) * a.m + ch0 + ch] = sum;
+                if (e < GROUPS && ch < chs) parts[(int64_t)(MATS == 1 ? 0 : second) * a.m + ch0 + ch] = sum;
             }
         }
     };
-    if (team == 0) results();
+    results();
     __syncthreads();
 
     if constexpr (!BACKWARD) {
