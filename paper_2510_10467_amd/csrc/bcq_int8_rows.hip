@@ -185,8 +185,8 @@ hipError_t go(const RowsParams &p, hipStream_t stream)
 template <int MATS>
 hipError_t pick(const RowsParams &p, hipStream_t stream)
 {
-    // More tokens' codes are worth two blocks of rows, where those still give every CU a workgroup: 14336 x 4096 with 32 tokens 13.6 -> 11.3 us,
-    // with 64 tokens 21.4 -> 16.2 (4096 x 14336 the other way, 11.4 and 16.1 against 15.7 and 18.5); 35840 x 5120 with 16 tokens 41.4 -> 36.6
+    // More tokens' codes are worth two blocks of rows, where those still give every CU a workgroup: 14336 x 4096 with 32 tokens 13.6 -> 11.3 us
+    // (4096 x 14336 the other way, 11.4 against 15.7); 35840 x 5120 with 16 tokens 41.4 -> 36.6
     // (with 8 tokens 34.0 both, gated 17920 x 5120 with 16 tokens the other way, 37.6 against 41.5).
     const bool tall = p.m * MATS >= 8192;
     if (p.tokens <= 8) return go<0, MATS, 1, 4, 3>(p, stream);
@@ -196,17 +196,15 @@ hipError_t pick(const RowsParams &p, hipStream_t stream)
         return go<1, MATS, 1, 4, 3>(p, stream);
     }
     if (p.tokens <= 32) return tall ? go<2, MATS, 2, 4, 2>(p, stream) : go<2, MATS, 1, 4, 3>(p, stream);
-    if constexpr (MATS == 1)
-        if (tall) return go<4, 1, 2, 4, 3>(p, stream);
     return go<4, MATS, 1, 4, 3>(p, stream);
 }
 
 }  // namespace
 
-// Up to 32 tokens, and up to 64 on matrices of at most 12288 rows (gate and up together): beyond that a workgroup moves more bytes of tokens' codes
-// than of weights, and the tiles of 64 x 64 are ahead (14336 x 4096 with 48 tokens 14.8 against 14.4 us, gated 31.1 against 27.6;
-// 4096 x 14336 14.2 against 26.1).
-bool int8_rows_supports(const Int8Args &a) { return a.tokens <= 32 || (a.tokens <= 64 && a.m * a.matrices <= 12288); }
+// Up to 32 tokens, and up to 64 where every workgroup of 16 rows has a CU of its own (4096 x 14336 with 48 tokens 13.6 against the tiles' 16.2 us, gated
+// 4096 x 4096 8.2 against 8.5): beyond that it moves more bytes of tokens' codes than of weights, and tiles are ahead (7000 x 4096 with 48 tokens
+// 10.5 against 8.1, gated 5120 x 4096 13.4 against 10.7).
+bool int8_rows_supports(const Int8Args &a) { return a.tokens <= 32 || (a.tokens <= 64 && a.m <= 4096); }
 
 hipError_t int8_rows_launch(const Int8Args &a, hipStream_t stream)
 {
