@@ -223,8 +223,8 @@ int bcq_quantize_form(const bcq_half *w, int p_low, int p_high, int cycles, int 
  * Shape rules: 1 <= m <= 2^24 (backward passes: 2^20), 16 <= n <= 131056, n % 16 == 0 (a sum of n products of two codes fits 32 bits),
  * 0 <= tokens <= 2^23, m * tokens <= 2^37, n * tokens <= 2^37.  q, w, x and dx must be 16-byte aligned, y, h, dy and dh 2-byte, scales 4-byte.
  * No tokens: the forward calls do nothing (their per-token pointers may be NULL), the backward calls write zeros to the scales' gradients.
- * Sums over columns are exact (32-bit integers), everything behind them is fp32, and results are rounded once to 16 bits.  Results do not depend
- * on what else is in the call's batch.
+ * Sums over columns are exact (32-bit integers), everything behind them is fp32, and results are rounded once to 16 bits.  A token's results of the
+ * forward calls are the same bits in every batch; no token's values touch another's dx.
  */
 typedef enum { BCQ_FLOAT16 = 0, BCQ_BFLOAT16 = 1 } bcq_type;
 typedef enum {
@@ -272,9 +272,9 @@ int bcq_int8_gated(const int8_t *q, const float *token_scales, const int8_t *w_g
  *   dx          [tokens][n] of `type` (written); gradients of the scales: float [m] (written)
  *   workspace   at least bcq_int8_backward_workspace(matrices, m, n, tokens) bytes, 256-byte aligned, contents irrelevant before
  *               and after; matrices: 1 for bcq_int8_gemm_backward, 2 for bcq_int8_gated_backward.  Calls that may run at the same time
- *               need one each.
- * The gradients of the projections are held in 11 bits on their way into the product with the weights, scaled per token so that dy's range does
- * not matter.  Sums have a fixed order: the same call gives the same bits.
+ *               need one each.  Fewer tokens may need more of it: ask for each number.
+ * The gradients of the projections are held in 11 bits on their way into the product with the weights, scaled per token so that the ranges of dy and
+ * of the activations do not matter.  Sums have a fixed order, which the sizes settle: the same call gives the same bits.
  * bcq_int8_backward_workspace returns BCQ_ERR_BAD_SHAPE for sizes that the calls refuse.  Host call.
  */
 int64_t bcq_int8_backward_workspace(int matrices, int64_t m, int64_t n, int64_t tokens);

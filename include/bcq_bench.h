@@ -82,7 +82,8 @@ int bcq_level_layout(int p, int row_blocks, int64_t n, int group, int with_offse
 
 /* Name of the variant the calling thread's most recent successful launch used ("" before any): "sign_select",
  * "lut", "plane_mfma" ("plane_mfma_rows" where that family ran in its row-streaming form: tall matrices with two to eight
- * requests, or with one request at one or two planes), "dequant_mfma", "plane_f16", "quantize". */
+ * requests, or with one request at one or two planes), "dequant_mfma", "plane_f16", "quantize"; of the 8-bit operators "int8_quantize", "int8_rows"
+ * (few tokens), "int8_tile", "int8_backward". */
 const char *bcq_last_kernel(void);
 
 /*

@@ -66,6 +66,19 @@ __device__ __forceinline__ float activate(float g, int activation, float &slope)
     return g * s;
 }
 
+// The backward passes hold a projection's gradients G in binary16, scaled so that a token's are of the order of 1 whatever dy, the token's scale and
+// the channels' are: times `norm`, the power of two that brings the token's largest |dy| to kPlainTop (one matrix: G = dy c) or kGatedTop, and over
+// the power of two next to what the other projection is typically made of, |token_scale| top 73 73 sqrt(n) (codes spread evenly have a mean
+// square of 73^2).  It is at most 128 128 n / (73 73 sqrt(n)) = 1113 times that, so with slopes of at most 1.13 a scaled G stays below
+// 2 kGatedTop 2 1113 1.13 = 40300: nothing overflows that has a number for its gradient.
+constexpr int kPlainTop = 9, kGatedTop = 3;             // exponents
+__device__ __forceinline__ float gradient_power(float norm, float token_scale, float top, float typical)
+{
+    const float size = fabsf(token_scale) * top * typical;              // (typical: 73 73 sqrt(n), or 0 for one matrix)
+    if (!(size > 0.f && size < __builtin_inff())) return norm;
+    return ldexpf(1.f, min(max(ilogbf(norm) - ilogbf(size), -120), 120));
+}
+
 hipError_t int8_quantize_launch(const uint16_t *x, bool bf16, int8_t *q, float *scales, int64_t rows, int64_t n, hipStream_t stream);
 
 // Few tokens: weights stream from memory into the matrix instructions' operands, without LDS.
@@ -82,6 +95,7 @@ struct Int8Workspace {
     int second_shape;               // ... and the tiles that they are taken in
     int64_t grad, norms, scale_top, parts, split_sums, bytes;       // offsets in bytes, and the whole
     int64_t part_count;             // room for so many partial sums of a channel
+    float typical;                  // what gradient_power counts with
 };
 Int8Workspace int8_workspace(int matrices, int64_t m, int64_t n, int64_t tokens);
 // the gradients of the projections, scaled as int8_backward_* explains, and partial sums of the channel scales' gradients

@@ -1,7 +1,8 @@
 // The backward passes of the 8-bit products, codes fixed: gradients of the activations and of the channel scales.
 //
-//   norms     per token the power of two f_t that brings its largest |dy| to [1/32, 1/16), and the power of two above all channel scales, S
-//   first     (bcq_int8_tile.hip) G = binary16 of f_t dg c / S for every channel of every matrix, and partial sums of dc
+//   norms     per token the power of two that brings its largest |dy| to a fixed size, and the power of two above all channel scales, S
+//   first     (bcq_int8_tile.hip) G = binary16 of f_t dg c / S for every channel of every matrix, and partial sums of dc; f_t: a power of two made of
+//             the token's norm and scale and S, which brings its G near 1 (gradient_power)
 //   second    dx = (S / f_t) sum over channels of G w: a product over the weights' ROWS
 //   finish    dc: the partial sums of a channel, in order; dx where the channels were taken in several runs: the runs' sums, in order
 //
@@ -13,6 +14,8 @@
 // What bounds it: the power of the matrix pipe on random operands (2048 tokens, 4096 columns, 2 x 14336 channels: 450 us = 1070 TFLOP/s, with gradients of
 // zero 389; the library's plain binary16 product of 8192^3 reaches 1300) and the codes' conversion (without it 400).  The whole gated
 // backward pass of that size: 743 us, of which the norms 12, the first half 290, the finish 5.
+#include <math.h>
+
 #include "bcq_int8.hpp"
 #include "bcq_internal.hpp"
 
@@ -26,7 +29,8 @@ typedef int v2i __attribute__((ext_vector_type(2)));
 
 // One workgroup per token, and a first one for the scales.  Four loads of a thread are under way at a time.
 __global__ __launch_bounds__(256) void int8_norms_kernel(const uint16_t *__restrict__ dy, const float *__restrict__ c0, const float *__restrict__ c1,
-                                                         float *__restrict__ norms, float *__restrict__ scale_top, int64_t m, bool bf16, bool whole)
+                                                         float *__restrict__ norms, float *__restrict__ scale_top, int64_t m, int exponent, bool bf16,
+                                                         bool whole)
 {
     __shared__ float tops[4];
     float top = 0.f;                                    // (a NaN leaves it as it is: such a token's results are NaN whatever its power)
@@ -73,9 +77,9 @@ __global__ __launch_bounds__(256) void int8_norms_kernel(const uint16_t *__restr
     if (threadIdx.x != 0) return;
     top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
     const bool usable = top > 0.f && top < __builtin_inff();
-    const int e = usable ? min(max(ilogbf(top), -120), 120) : 0;
+    const int e = usable ? min(max(ilogbf(top), -110), 110) : 0;
     if (for_scales) *scale_top = ldexpf(1.f, usable ? e + 1 : 0);
-    else norms[token] = ldexpf(1.f, usable ? -5 - e : 0);
+    else norms[token] = ldexpf(1.f, usable ? exponent - e : 0);
 }
 
 constexpr uint32_t kTokenGroup = 4;       // token tiles whose workgroups run beside each other for a column tile
@@ -83,7 +87,8 @@ constexpr uint32_t kTokenGroup = 4;       // token tiles whose workgroups run be
 struct SecondParams {
     const _Float16 *grad;
     const int8_t *w[2];
-    const float *norms, *scale_top;
+    const float *norms, *token_scales, *scale_top;
+    float typical;
     uint16_t *dx;
     uint32_t m, m_padded, n, tokens, grad_stride;
     uint32_t column_tiles, token_tiles;
@@ -319,7 +324,8 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_second_kernel(const Sec
 #pragma unroll
     for (int t = 0; t < (team == 0 ? S::FT : 0); ++t) {
         const uint32_t tok = (wt * S::FT + t) * 32 + r32;
-        const float back = top / a.norms[t0 + min(tok, toks - 1)];      // (powers of two)
+        const uint32_t at = t0 + min(tok, toks - 1);
+        const float back = top / gradient_power(a.norms[at], a.token_scales[at], top, a.typical);       // (powers of two)
 #pragma unroll
         for (int c = 0; c < S::FC; ++c)
 #pragma unroll
@@ -343,7 +349,8 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_second_kernel(const Sec
 // What is left, in one launch: the first sums_blocks workgroups add up the partial sums of the scales' gradients, in order, a channel a thread and eight
 // under way at a time; the others the runs' sums of dx, four columns a thread.
 struct FinishParams {
-    const float *parts, *split_sums, *norms, *scale_top;
+    const float *parts, *split_sums, *norms, *token_scales, *scale_top;
+    float typical;
     float *dscales[2];
     uint16_t *dx;
     int64_t m, part_count, tokens;
@@ -376,7 +383,8 @@ __global__ __launch_bounds__(64) void int8_finish_kernel(const FinishParams a)
     v4f sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int s = 0; s < a.splits; ++s) sum += reinterpret_cast<const v4f *>(a.split_sums)[s * count + i];
-    const float back = *a.scale_top / a.norms[i * 4 / a.n];             // (powers of two)
+    const int64_t token = i * 4 / a.n;
+    const float top = *a.scale_top, back = top / gradient_power(a.norms[token], a.token_scales[token], top, a.typical);     // (powers of two)
     uint32_t out[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) out[k] = to_16(sum[k] * back, a.bf16);
@@ -423,7 +431,7 @@ SecondPlan second_plan(int matrices, int64_t m, int64_t n, int64_t tokens)
         const int64_t tiles = ((n + S::COLS - 1) / S::COLS) * ((tokens + S::TOKS - 1) / S::TOKS);
         for (int splits = 1; splits <= 16; ++splits) {
             const int64_t run = (steps + splits - 1) / splits, each = (tiles * splits + 255) / 256;
-            if (splits > 1 && run < 4) break;
+            if (splits > 1 && (run < 4 || tokens * n > int64_t(1) << 32)) break;        // (the finish counts its threads in 32 bits)
             const float us = (float)(run + 4) * (each <= 1 ? alone : (float)each * shared) +
                              (splits > 1 ? 1.f + (float)splits * (float)tokens * (float)n * (8.f / 8e6f) : 0.f);
             if (best == 0.f || us < best) {
@@ -447,6 +455,7 @@ Int8Workspace int8_workspace(int matrices, int64_t m, int64_t n, int64_t tokens)
     const SecondPlan plan = second_plan(matrices, m, n, tokens);
     ws.second_shape = plan.shape;
     ws.splits = plan.splits;
+    ws.typical = matrices == 1 ? 0.f : 73.f * 73.f * sqrtf((float)n);
     ws.grad = 0;
     ws.norms = up(tokens * ws.grad_stride * 2);
     ws.scale_top = ws.norms + up(tokens * 4);
@@ -465,6 +474,8 @@ hipError_t int8_backward_launch(const Int8Args &a, hipStream_t stream)
     f.parts = reinterpret_cast<const float *>(base + ws.parts);
     f.split_sums = reinterpret_cast<const float *>(base + ws.split_sums);
     f.norms = norms;
+    f.token_scales = a.token_scales;
+    f.typical = ws.typical;
     f.scale_top = scale_top;
     f.dscales[0] = a.dscales[0];
     f.dscales[1] = a.dscales[a.matrices - 1];
@@ -479,7 +490,8 @@ hipError_t int8_backward_launch(const Int8Args &a, hipStream_t stream)
     if (a.tokens > 0) {
         const bool whole = a.m % 8 == 0 && (reinterpret_cast<uintptr_t>(a.dy) & 15) == 0;
         hipLaunchKernelGGL(int8_norms_kernel, dim3((unsigned)(a.tokens + 1)), dim3(256), 0, stream, a.dy, a.channel_scales[0],
-                           a.channel_scales[a.matrices - 1], norms, scale_top, a.m, a.bf16, whole);
+                           a.channel_scales[a.matrices - 1], norms, scale_top, a.m,
+                           a.matrices == 1 ? kPlainTop : kGatedTop, a.bf16, whole);
         if (hipError_t e = hipGetLastError()) return e;
         if (hipError_t e = int8_tile_backward_launch(a, ws, stream, f.part_count)) return e;
         SecondParams p{};
@@ -487,6 +499,8 @@ hipError_t int8_backward_launch(const Int8Args &a, hipStream_t stream)
         p.w[0] = a.w[0];
         p.w[1] = a.w[a.matrices - 1];
         p.norms = norms;
+        p.token_scales = a.token_scales;
+        p.typical = ws.typical;
         p.scale_top = scale_top;
         p.dx = a.dx;
         p.m = (uint32_t)a.m;

@@ -36,6 +36,7 @@ struct TileParams {
     // backward
     const uint16_t *dy;
     const float *norms, *scale_top;
+    float typical;
     _Float16 *grad;                 // [tokens][grad_stride]: matrix k from k * m_padded on
     uint32_t grad_stride, m_padded;
     float *parts;                   // [token_tiles * WT][matrices][m]
@@ -320,7 +321,7 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_tile_kernel(const TileP
     [[maybe_unused]] float *norms = token_scales + S::TOKS;
     for (uint32_t i = threadIdx.x; i < S::TOKS; i += S::WAVES * 64) {
         token_scales[i] = i < toks ? a.token_scales[t0 + i] : 0.f;
-        if constexpr (BACKWARD) norms[i] = i < toks ? a.norms[t0 + i] : 1.f;
+        if constexpr (BACKWARD) norms[i] = i < toks ? gradient_power(a.norms[t0 + i], token_scales[i], *a.scale_top, a.typical) : 1.f;
     }
     if constexpr (BACKWARD) {
         if (a.whole) {
@@ -386,10 +387,10 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_tile_kernel(const TileP
                             } else {
                                 // (channels and tokens past the end have a gradient and a scale of 0)
                                 const float d = from_16((i & 1) ? dy[i >> 1] >> 16 : dy[i >> 1] & 0xffffu, a.bf16);
-                                // The gradients that the second half multiplies are held in binary16 (11 bits): a token's by the power of
-                                // two that brings its largest dy to about 1/32, times its channel's scale over the power of two above
-                                // all scales, so that neither the type's range nor the scales' sizes matter.  A value is off by
-                                // 2^-12 of itself, as much as by a result's last rounding.
+                                // The gradients that the second half multiplies are held in binary16 (11 bits): times the token's power of
+                                // two (gradient_power) and the channel's scale over the power of two above all scales.  A value is off by 2^-12
+                                // of itself, as much as by a result's last rounding, or by 2^-25 of what is of the order of the
+                                // token's largest.
                                 if constexpr (MATS == 1) {
                                     out[i] = to_16(d * (norm * (c0[i] * inv_top)), false);
                                     sums[(r - r0) * 16 + 4 * e + i] += d * p;
@@ -543,6 +544,7 @@ hipError_t int8_tile_backward_launch(const Int8Args &a, const Int8Workspace &ws,
     p.grad = reinterpret_cast<_Float16 *>(base + ws.grad);
     p.norms = reinterpret_cast<const float *>(base + ws.norms);
     p.scale_top = reinterpret_cast<const float *>(base + ws.scale_top);
+    p.typical = ws.typical;
     p.parts = reinterpret_cast<float *>(base + ws.parts);
     p.grad_stride = (uint32_t)ws.grad_stride;
     p.m_padded = (uint32_t)(ws.grad_stride / a.matrices);

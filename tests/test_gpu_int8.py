@@ -240,6 +240,19 @@ def test_a_token_does_not_touch_another(bcq, tokens):
     assert torch.equal(y[3:4].sign(), sums.sign().half())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_token_in_batches_of_any_size(bcq, dtype):
+    """The same bits for a token alone and among few and many others, whichever kernels and tiles those take."""
+    gen = generator("batches")
+    q, ts, [(wg, cg), (wu, cu)] = operands(600, 4200, 400, gen, 2)
+    calls = [lambda q, ts: bcq.bcq_int8_gemm(q, ts, wg, cg, dtype), *(
+        lambda q, ts, act=act: bcq.bcq_int8_gated(q, ts, wg, cg, wu, cu, act, dtype) for act in ("silu", "gelu"))]
+    for call in calls:
+        whole = call(q, ts)
+        for tokens in (1, 5, 12, 30, 33, 64, 100, 200, 300):
+            assert torch.equal(call(q[:tokens], ts[:tokens]), whole[:tokens]), tokens
+
+
 @pytest.mark.parametrize("tokens, m, n", [(1, 256, 512), (40, 300, 512)])
 def test_results_of_any_alignment(bcq, tokens, m, n):
     gen = generator("align", tokens)
@@ -287,11 +300,17 @@ def second_half_error(err, grads, cs, w, top, norm):
     return each @ w.abs() + (k / 16 + 24) * E32 * ((grads * cs).abs() @ w.abs())
 
 
-def powers(dy, *cs):
+def powers(dy, *cs, ts=None, n=0):
+    """The powers of two that the gradients are held at: above all channel scales, and a token's: its largest |dy| to 2^9, or, gated (ts, n), to 2^3
+    times what undoes the size of its projections."""
     top = max(float(c.abs().max()) for c in cs)
     top = 2.0 ** (math.floor(math.log2(top)) + 1)
     most = dy.double().abs().amax(dim=1)
-    norm = torch.where(most > 0, torch.exp2(-5 - torch.floor(torch.log2(most.clamp_min(1e-300)))), torch.ones_like(most))
+    largest = 9 if ts is None else 3
+    norm = torch.where(most > 0, torch.exp2(largest - torch.floor(torch.log2(most.clamp_min(1e-300)))), torch.ones_like(most))
+    if ts is not None:
+        size = (ts.abs() * top) * (torch.tensor(73.0 * 73.0, dtype=torch.float32) * torch.tensor(float(n), dtype=torch.float32).sqrt()).item()
+        norm = norm * torch.exp2(-torch.floor(torch.log2(size.double())))
     return top, norm
 
 
@@ -337,11 +356,39 @@ def test_gated_backward(bcq, dtype, activation, tokens, m, n):
     close(dgate, (dg * pg).sum(dim=0), sums_error(dg * pg, (dg_err + 4 * E32 * dg.abs()) * pg.abs(), tokens) + 1e-40, "dgate_scales")
     close(dup, (du * pu).sum(dim=0), sums_error(du * pu, (du_err + 4 * E32 * du.abs()) * pu.abs(), tokens) + 1e-40, "dup_scales")
     ref = (dg * cg.double()) @ wg.double() + (du * cu.double()) @ wu.double()
-    top, norm = powers(dh, cg, cu)
+    top, norm = powers(dh, cg, cu, ts=ts, n=n)
     tol = second_half_error(dg_err, dg, cg.double(), wg.double(), top, norm) + second_half_error(du_err, du, cu.double(), wu.double(), top, norm)
     close(dx, ref, 1.01 * tol + ref.abs() * half_step(dtype) + tiny(dtype), "dx")
     again = bcq.bcq_int8_gated_backward(dh, q, ts, wg, cg, wu, cu, activation)
     assert all(torch.equal(a, b) for a, b in zip(again, (dx, dgate, dup)))
+
+
+@pytest.mark.parametrize("activation", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens, m, n", [(24, 200, 272), (24, 64, 4112)])
+def test_gradients_of_small_and_large_activations(bcq, dtype, activation, tokens, m, n):
+    """A token's gradients have the precision of their own size, whatever its activations' is: those of 2^-18 of the others too."""
+    gen = generator("small", tokens, m, n)
+    q, ts, [(wg, cg), (wu, cu)] = operands(tokens, m, n, gen, 2)
+    ts = ts * torch.exp2(torch.arange(tokens, device="cuda") - 18.0)         # 2^-18 .. 2^5
+    dh = torch.randn((tokens, m), device="cuda", generator=gen).clamp(-4, 4).to(dtype)
+    dx, dgate, dup = bcq.bcq_int8_gated_backward(dh, q, ts, wg, cg, wu, cu, activation)
+    d = dh.double()
+    pg, pu = (sums64(q, w) * ts.double()[:, None] for w in (wg, wu))
+    g, u = pg * cg.double(), pu * cu.double()
+    act, slope, sig, z, inner = act64(g, activation)
+    arg = 16 * z.abs() + 24
+    slope_err = E32 * (arg * (sig + g.abs() * sig * (1 - sig) * inner) + 6 * g.abs() * sig * inner)
+    dg, du = d * u * slope, d * act
+    dg_err, du_err = (d * u).abs() * slope_err + 8 * E32 * dg.abs(), du.abs() * arg * E32
+    ref = (dg * cg.double()) @ wg.double() + (du * cu.double()) @ wu.double()
+    # a gradient is off by 2^-11 of itself or, far below its token's, by 2^-25 of about the token's size: all together 2^-9 of the root of the squares'
+    # sum times the codes' 73, six times over what independent roundings make
+    of_token = ((dg * cg.double()).square().sum(dim=1) + (du * cu.double()).square().sum(dim=1)).sqrt() * 73
+    assert bool(((dx.double() - ref).abs() <= of_token[:, None] * 2.0 ** -9 + ref.abs() * half_step(dtype) + tiny(dtype)).all())
+    top, norm = powers(dh, cg, cu, ts=ts, n=n)
+    tol = second_half_error(dg_err, dg, cg.double(), wg.double(), top, norm) + second_half_error(du_err, du, cu.double(), wu.double(), top, norm)
+    close(dx, ref, 1.01 * tol + ref.abs() * half_step(dtype) + tiny(dtype), "dx")
 
 
 def test_gradients_against_differences(bcq):
