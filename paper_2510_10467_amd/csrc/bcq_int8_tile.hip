@@ -13,8 +13,8 @@
 // Neighbouring workgroups' numbers go to different XCDs, each with a cache of its own: they are renumbered so that one XCD works on
 // the token tiles of the same weights.
 //
-// What bounds it: with every CU at work on large tiles the clock that the matrix pipe's power leaves (28672 x 8192 with 2048 tokens 461 us = 2090 TOP/s,
-// with codes of zero 415; the library's own 8-bit product of 8192^3 2100).  With few tiles the latency of a step, about 0.3 us where three
+// What bounds it: with every CU at work on large tiles the clock that the matrix pipe's power leaves (28672 x 8192 with 2048 tokens 445 us = 2160 TOP/s;
+// the library's own 8-bit product of 8192^3 2100; without the tiles of the last half round 465, with codes of zero 415).  With few tiles the latency of a step, about 0.3 us where three
 // steps of 64 x 64 are under way.  Tall matrices with 33 to 128 tokens: the tiles of the last round, and the
 // weights' half of the bytes under way (17920 x 5120 gated with 48 tokens 47 us = 3.9 TB/s, with one token 33).
 #include <type_traits>
@@ -25,12 +25,17 @@
 namespace bcq {
 namespace {
 
+// Channels from first_channel on, in row_tiles times token_tiles tiles
+struct TilePart {
+    uint32_t first_channel, row_tiles, token_tiles;
+};
+
 struct TileParams {
     const int8_t *q, *w[2];
     const float *token_scales, *channel_scales[2];
     uint16_t *y;
     uint32_t m, n, tokens;
-    uint32_t row_tiles, token_tiles;
+    TilePart part[2];               // a launch's first workgroups, and in mixed launches those behind them
     int activation;
     bool bf16, whole;               // whole: rows of y and dy are in pieces of 16 bytes
     // backward
@@ -39,7 +44,7 @@ struct TileParams {
     float typical;
     _Float16 *grad;                 // [tokens][grad_stride]: matrix k from k * m_padded on
     uint32_t grad_stride, m_padded;
-    float *parts;                   // [token_tiles * WT][matrices][m]
+    float *parts;                   // [a wave's tokens, from the first on][matrices][m]
 };
 
 // FR x FT tiles of 32 x 32 in a wave, WR x WT waves in a team, RING buffers of each team
@@ -105,8 +110,9 @@ __device__ __forceinline__ float sums_of_32(float (&v)[32], int lane)
     return v[0];
 }
 
+// Workgroup `block` of a part.
 template <typename S, int MATS, bool BACKWARD, int ACT>
-__global__ __launch_bounds__(S::WAVES * 64, 2) void int8_tile_kernel(const TileParams a)
+__device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, uint32_t block)
 {
     using L = TileLds<S, MATS, BACKWARD>;
     constexpr int FRC = S::FR / MATS;                       // tiles of 32 channels in a wave
@@ -119,13 +125,13 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_tile_kernel(const TileP
     const int r32 = lane & 31, half = lane >> 5;
 
     // the tile: first by XCD, then in groups of up to eight token tiles, the tokens of a group running fastest
-    const uint32_t total = gridDim.x, xcd = blockIdx.x & 7;
-    const uint32_t id = xcd * (total >> 3) + min(xcd, total & 7) + (blockIdx.x >> 3);
-    const uint32_t group = id / (8 * a.row_tiles);
-    const uint32_t in_group = min(8u, a.token_tiles - group * 8);
-    const uint32_t rest = id - group * 8 * a.row_tiles;
+    const uint32_t total = part.row_tiles * part.token_tiles, xcd = block & 7;
+    const uint32_t id = xcd * (total >> 3) + min(xcd, total & 7) + (block >> 3);
+    const uint32_t group = id / (8 * part.row_tiles);
+    const uint32_t in_group = min(8u, part.token_tiles - group * 8);
+    const uint32_t rest = id - group * 8 * part.row_tiles;
     const uint32_t row_tile = rest / in_group, token_tile = group * 8 + rest % in_group;
-    const uint32_t ch0 = row_tile * CHANNELS, t0 = token_tile * S::TOKS;
+    const uint32_t ch0 = part.first_channel + row_tile * CHANNELS, t0 = token_tile * S::TOKS;
 
     const uint32_t chs = min((uint32_t)CHANNELS, a.m - ch0), toks = min((uint32_t)S::TOKS, a.tokens - t0);
     const int8_t *const q_base = a.q + (int64_t)t0 * a.n;
@@ -449,16 +455,55 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_tile_kernel(const TileP
 }
 
 template <typename S, int MATS, bool BACKWARD, int ACT>
-hipError_t go(TileParams p, hipStream_t stream, int64_t *part_count)
+__global__ __launch_bounds__(S::WAVES * 64, 2) void int8_tile_kernel(const TileParams a)
 {
-    using L = TileLds<S, MATS, BACKWARD>;
-    p.row_tiles = (p.m + L::CHANNELS - 1) / L::CHANNELS;
-    p.token_tiles = (p.tokens + S::TOKS - 1) / S::TOKS;
-    if (part_count) *part_count = (int64_t)p.token_tiles * S::WT;
-    const auto kernel = int8_tile_kernel<S, MATS, BACKWARD, ACT>;
-    if (hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), L::BYTES)) return e;
-    hipLaunchKernelGGL(kernel, dim3(p.row_tiles * p.token_tiles), dim3(S::WAVES * 64), L::BYTES, stream, p);
+    tile<S, MATS, BACKWARD, ACT>(a, a.part[0], blockIdx.x);
+}
+
+// Two shapes in one launch: the second's workgroups are behind the first's.
+template <typename S, typename S2, int MATS, bool BACKWARD, int ACT>
+__global__ __launch_bounds__(S::WAVES * 64, 2) void int8_tiles_kernel(const TileParams a)
+{
+    static_assert(S::WAVES == S2::WAVES, "one size of workgroup");
+    const uint32_t first = a.part[0].row_tiles * a.part[0].token_tiles;
+    if (blockIdx.x < first) tile<S, MATS, BACKWARD, ACT>(a, a.part[0], blockIdx.x);
+    else tile<S2, MATS, BACKWARD, ACT>(a, a.part[1], blockIdx.x - first);
+}
+
+hipError_t launch(void (*kernel)(const TileParams), int lds_bytes, int waves, const TileParams &p, hipStream_t stream)
+{
+    if (hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), lds_bytes)) return e;
+    const uint32_t tiles = p.part[0].row_tiles * p.part[0].token_tiles + p.part[1].row_tiles * p.part[1].token_tiles;
+    hipLaunchKernelGGL(kernel, dim3(tiles), dim3(waves * 64), lds_bytes, stream, p);
     return hipGetLastError();
+}
+
+template <typename S, int MATS>
+TilePart part_of(uint32_t first_channel, uint32_t channels, uint32_t tokens)
+{
+    constexpr uint32_t CHANNELS = S::ROWS / MATS;
+    return {first_channel, (channels + CHANNELS - 1) / CHANNELS, (tokens + S::TOKS - 1) / S::TOKS};
+}
+
+template <typename S, int MATS, bool BACKWARD, int ACT>
+hipError_t go(TileParams p, hipStream_t stream, int64_t &part_count)
+{
+    part_count = (p.tokens + S::FT * 32 - 1) / (S::FT * 32);
+    p.part[0] = part_of<S, MATS>(0, p.m, p.tokens);
+    return launch(int8_tile_kernel<S, MATS, BACKWARD, ACT>, TileLds<S, MATS, BACKWARD>::BYTES, S::WAVES, p, stream);
+}
+
+// Full rounds of 256 workgroups of the first shape, for what is left the second.
+template <typename S, typename S2, int MATS, bool BACKWARD, int ACT>
+hipError_t go_mixed(TileParams p, uint32_t first_row_tiles, hipStream_t stream, int64_t &part_count)
+{
+    static_assert(S::FT == S2::FT, "partial sums over as many tokens");
+    part_count = (p.tokens + S::FT * 32 - 1) / (S::FT * 32);
+    constexpr uint32_t CHANNELS = S::ROWS / MATS;
+    constexpr int BYTES = TileLds<S, MATS, BACKWARD>::BYTES, BYTES2 = TileLds<S2, MATS, BACKWARD>::BYTES;
+    p.part[0] = part_of<S, MATS>(0, first_row_tiles * CHANNELS, p.tokens);
+    p.part[1] = part_of<S2, MATS>(first_row_tiles * CHANNELS, p.m - first_row_tiles * CHANNELS, p.tokens);
+    return launch(int8_tiles_kernel<S, S2, MATS, BACKWARD, ACT>, BYTES > BYTES2 ? BYTES : BYTES2, S::WAVES, p, stream);
 }
 
 // What a workgroup takes per 128 columns, alone on its CU and as one of several in turn (microseconds, measured): the shape that is expected to be done
@@ -466,11 +511,14 @@ hipError_t go(TileParams p, hipStream_t stream, int64_t *part_count)
 // keep enough bytes under way where there are few.  (4096 columns: 4096 rows and 256 tokens 52 / 31 / 20 / 22 / 15 / 11 / 15 us from the first shape to the last,
 // 14336 rows and 512 tokens, gated, 65 / 75 / 90 / 106 / 131 / 162.  5120 columns, 17920 rows and 48 tokens, gated: 78 / 56 / 62 / 47 / 65 / 52.  4096 x 4096 with 100 tokens:
 // the last two 10.4 and 8.1.)
+using Largest = TileShape<2, 4, 4, 2, 2>;
+using Large = TileShape<4, 2, 2, 2, 3>;
+constexpr float kLargestUs = 1.70f, kLargeUs = 1.08f;
 template <int MATS, bool BACKWARD, typename F>
 void for_shapes(F f)
 {
-    f(TileShape<2, 4, 4, 2, 2>{}, 1.70f, 1.70f);            // 256 x 256
-    f(TileShape<4, 2, 2, 2, 3>{}, 1.08f, 1.10f);            // 256 x 128
+    f(Largest{}, kLargestUs, kLargestUs);                   // 256 x 256
+    f(Large{}, kLargeUs, 1.10f);                            // 256 x 128
     f(TileShape<2, 2, 2, 2, 4>{}, 0.60f, 0.62f);            // 128 x 128
     f(TileShape<4, 1, 2, 2, 4>{}, 0.69f, 0.70f);            // 256 x 64
     f(TileShape<2, 1, 2, 2, 6, 2, 64>{}, 0.34f, 0.50f);     // 128 x 64, two teams
@@ -480,8 +528,8 @@ void for_shapes(F f)
     }
 }
 
-template <int MATS, bool BACKWARD>
-hipError_t pick(const TileParams &p, hipStream_t stream, int64_t *part_count = nullptr)
+template <int MATS, bool BACKWARD, int ACT>
+hipError_t pick(const TileParams &p, hipStream_t stream, int64_t &part_count)
 {
     float best = 0.f;
     int index = 0, chosen = -1;
@@ -496,16 +544,29 @@ hipError_t pick(const TileParams &p, hipStream_t stream, int64_t *part_count = n
         }
         ++index;
     });
+    // The largest tiles as far as they fill rounds, and where one round of those of half the tokens takes what is left, that (2048 tokens, 4096
+    // columns, gated, 14336 rows, 3.5 rounds: 247 -> 231 us; 12288 rows, three rounds: 189).
+    const TilePart all = part_of<Largest, MATS>(0, p.m, p.tokens);
+    const int64_t rounds = (int64_t)all.row_tiles * all.token_tiles / 256;
+    const uint32_t first = (uint32_t)(rounds * 256 / all.token_tiles);
+    if (rounds > 0 && first < all.row_tiles) {
+        const TilePart left = part_of<Large, MATS>(0, (all.row_tiles - first) * (Largest::ROWS / MATS), p.tokens);
+        if ((int64_t)left.row_tiles * left.token_tiles <= 256 && (float)rounds * kLargestUs + kLargeUs < best)
+            return go_mixed<Largest, Large, MATS, BACKWARD, ACT>(p, first, stream, part_count);
+    }
     hipError_t result = hipErrorInvalidValue;
     index = 0;
     for_shapes<MATS, BACKWARD>([&](auto shape, float, float) {
-        if (index++ == chosen) {
-            using S = decltype(shape);
-            if (MATS == 2 && p.activation == BCQ_ACT_GELU) result = go<S, MATS, BACKWARD, MATS == 2 ? BCQ_ACT_GELU : BCQ_ACT_SILU>(p, stream, part_count);
-            else result = go<S, MATS, BACKWARD, BCQ_ACT_SILU>(p, stream, part_count);
-        }
+        if (index++ == chosen) result = go<decltype(shape), MATS, BACKWARD, ACT>(p, stream, part_count);
     });
     return result;
+}
+
+template <bool BACKWARD>
+hipError_t pick(const TileParams &p, int matrices, hipStream_t stream, int64_t &part_count)
+{
+    if (matrices == 1) return pick<1, BACKWARD, BCQ_ACT_SILU>(p, stream, part_count);
+    return p.activation == BCQ_ACT_GELU ? pick<2, BACKWARD, BCQ_ACT_GELU>(p, stream, part_count) : pick<2, BACKWARD, BCQ_ACT_SILU>(p, stream, part_count);
 }
 
 TileParams params(const Int8Args &a)
@@ -533,8 +594,8 @@ TileParams params(const Int8Args &a)
 
 hipError_t int8_tile_launch(const Int8Args &a, hipStream_t stream)
 {
-    const TileParams p = params(a);
-    return a.matrices == 2 ? pick<2, false>(p, stream) : pick<1, false>(p, stream);
+    int64_t part_count;
+    return pick<false>(params(a), a.matrices, stream, part_count);
 }
 
 hipError_t int8_tile_backward_launch(const Int8Args &a, const Int8Workspace &ws, hipStream_t stream, int64_t &part_count)
@@ -548,7 +609,7 @@ hipError_t int8_tile_backward_launch(const Int8Args &a, const Int8Workspace &ws,
     p.parts = reinterpret_cast<float *>(base + ws.parts);
     p.grad_stride = (uint32_t)ws.grad_stride;
     p.m_padded = (uint32_t)(ws.grad_stride / a.matrices);
-    return a.matrices == 2 ? pick<2, true>(p, stream, &part_count) : pick<1, true>(p, stream, &part_count);
+    return pick<true>(p, a.matrices, stream, part_count);
 }
 
 }  // namespace bcq
