@@ -11,9 +11,10 @@
 // 8-bit values delivers (16 lanes take eight rows of 16 columns), and turns them into binary16, exactly: a code's byte
 // with its sign bit turned under the byte 0x64 is the number 1024 + 128 + code.
 //
-// What bounds it: the power of the matrix pipe on random operands (2048 tokens, 4096 columns, 2 x 14336 channels: 450 us = 1070 TFLOP/s, with gradients of
-// zero 389; the library's plain binary16 product of 8192^3 reaches 1300) and the codes' conversion (without it 400).  The whole gated
-// backward pass of that size: 743 us, of which the norms 12, the first half 290, the finish 5.
+// What bounds it: the power of the matrix pipe on random operands (2048 tokens, 4096 columns, 2 x 14336 channels: 437 to 459 us = 1100 to 1050 TFLOP/s,
+// with gradients of zero 330; the library's plain binary16 product of 8192^3 1300), the codes' conversion beside it, and with few tokens
+// the weights' bytes (17920 x 5120, gated, 48 tokens: 47 us = 3.9 TB/s).  The whole gated backward pass of 2048 tokens: 700 us, of which the
+// norms 13, the first half 290, the finish 5.
 #include <math.h>
 
 #include "bcq_int8.hpp"

@@ -14,9 +14,10 @@
 // the token tiles of the same weights.
 //
 // What bounds it: with every CU at work on large tiles the clock that the matrix pipe's power leaves (28672 x 8192 with 2048 tokens 445 us = 2160 TOP/s;
-// the library's own 8-bit product of 8192^3 2100; without the tiles of the last half round 465, with codes of zero 415).  With few tiles the latency of a step, about 0.3 us where three
-// steps of 64 x 64 are under way.  Tall matrices with 33 to 128 tokens: the tiles of the last round, and the
-// weights' half of the bytes under way (17920 x 5120 gated with 48 tokens 47 us = 3.9 TB/s, with one token 33).
+// the library's own 8-bit product of 8192^3 2100; with codes of zero a tenth less time).  With fewer tiles what LDS takes and gives: a KiB written
+// by a load takes it 16 cycles, a KiB of operands read 8.  With few tiles the latency of a step, about 0.3 us where three steps of
+// 64 x 64 are under way.  Tall matrices with 33 to 128 tokens: the CUs that the last round leaves without work, and the weights' share of
+// the bytes under way (17920 x 5120 gated with 48 tokens 47 us = 3.9 TB/s, with one token 33).
 #include <type_traits>
 
 #include "bcq_int8.hpp"
@@ -65,7 +66,7 @@ struct TileLds {
     static constexpr int CHANNELS = S::ROWS / MATS;
     static constexpr int OUT_ROW = CHANNELS * 2 + 16;
     static constexpr int OUT = S::TOKS * OUT_ROW;           // one 16-bit result tile
-    static constexpr int DY_EACH = S::TOKS * CHANNELS / 8 / (S::WAVES * 64);       // pieces of dy's tile for each thread
+    static constexpr int DY_EACH = (S::TOKS * CHANNELS / 8 + S::WAVES * 64 - 1) / (S::WAVES * 64);     // pieces of dy's tile for each thread, at most
     static constexpr int OUTS = BACKWARD ? MATS : 1;
     static constexpr int SCALES = OUTS * OUT;               // the channels' scales behind them
     static constexpr int TOKEN_SCALES = SCALES + MATS * CHANNELS * 4;       // the tokens' scales, and their powers of two
@@ -117,7 +118,7 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
     using L = TileLds<S, MATS, BACKWARD>;
     constexpr int FRC = S::FR / MATS;                       // tiles of 32 channels in a wave
     constexpr int CHANNELS = L::CHANNELS;
-    static_assert(!BACKWARD || CHANNELS % 64 == 0, "the last tile writes the gradients' rows to their end");
+    static_assert(!BACKWARD || CHANNELS % 64 == 0 || CHANNELS == 32, "the last tile writes the gradients' rows to their end");
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int team = wave / S::TEAM_WAVES, tw = wave % S::TEAM_WAVES;
@@ -160,7 +161,6 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
     constexpr int PIECES = CHANNELS / 8, THREADS = S::WAVES * 64;           // 16-byte pieces of a tile's row
     [[maybe_unused]] u32x4 dy_early[BACKWARD ? L::DY_EACH : 1];
     if constexpr (BACKWARD) {
-        static_assert(L::DY_EACH * THREADS == S::TOKS * PIECES && S::TOKS * CHANNELS % (8 * THREADS) == 0, "the same for every thread");
         if (a.whole) {
 #pragma unroll
             for (int k = 0; k < L::DY_EACH; ++k) {
@@ -334,7 +334,7 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
 #pragma unroll
             for (int k = 0; k < L::DY_EACH; ++k) {
                 const uint32_t i = threadIdx.x + k * THREADS;
-                *reinterpret_cast<u32x4 *>(lds + i / PIECES * L::OUT_ROW + i % PIECES * 16) = dy_early[k];
+                if (i < S::TOKS * PIECES) *reinterpret_cast<u32x4 *>(lds + i / PIECES * L::OUT_ROW + i % PIECES * 16) = dy_early[k];
             }
         } else {
             for (int i = threadIdx.x; i < S::TOKS * CHANNELS; i += 8 * THREADS) {
@@ -346,7 +346,8 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
                 }
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
-                    *reinterpret_cast<uint16_t *>(lds + (i + k * THREADS) / CHANNELS * L::OUT_ROW + (i + k * THREADS) % CHANNELS * 2) = v[k];
+                    if (i + k * THREADS < S::TOKS * CHANNELS)
+                        *reinterpret_cast<uint16_t *>(lds + (i + k * THREADS) / CHANNELS * L::OUT_ROW + (i + k * THREADS) % CHANNELS * 2) = v[k];
             }
         }
     }
@@ -450,6 +451,9 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
             if (tok < toks && ch0 + piece * 8 < a.m_padded)
                 *reinterpret_cast<u32x4 *>(a.grad + (int64_t)(t0 + tok) * a.grad_stride + k * a.m_padded + ch0 + piece * 8) =
                     *reinterpret_cast<const u32x4 *>(lds + k * L::OUT + tok * L::OUT_ROW + piece * 16);
+            if constexpr (CHANNELS < 64)                    // (its last 32 channels may be the gradients' last but 32)
+                if (tok < toks && ch0 + CHANNELS >= a.m && ch0 + CHANNELS < a.m_padded)
+                    *reinterpret_cast<u32x4 *>(a.grad + (int64_t)(t0 + tok) * a.grad_stride + k * a.m_padded + ch0 + CHANNELS + piece * 8) = u32x4{0, 0, 0, 0};
         }
     }
 }
@@ -514,7 +518,7 @@ hipError_t go_mixed(TileParams p, uint32_t first_row_tiles, hipStream_t stream, 
 using Largest = TileShape<2, 4, 4, 2, 2>;
 using Large = TileShape<4, 2, 2, 2, 3>;
 constexpr float kLargestUs = 1.70f, kLargeUs = 1.08f;
-template <int MATS, bool BACKWARD, typename F>
+template <typename F>
 void for_shapes(F f)
 {
     f(Largest{}, kLargestUs, kLargestUs);                   // 256 x 256
@@ -522,10 +526,8 @@ void for_shapes(F f)
     f(TileShape<2, 2, 2, 2, 4>{}, 0.60f, 0.62f);            // 128 x 128
     f(TileShape<4, 1, 2, 2, 4>{}, 0.69f, 0.70f);            // 256 x 64
     f(TileShape<2, 1, 2, 2, 6, 2, 64>{}, 0.34f, 0.50f);     // 128 x 64, two teams
-    if constexpr (!BACKWARD || MATS == 1) {                 // (a tile of the gated backward pass has 64 channels or more, as the gradients' rows have)
-        f(TileShape<1, 2, 2, 1, 4, 2>{}, 0.28f, 0.30f);     // 64 x 64, two teams
-        f(TileShape<1, 1, 2, 1, 3, 4>{}, 0.20f, 0.20f);     // 64 x 32, four teams
-    }
+    f(TileShape<1, 2, 2, 1, 4, 2>{}, 0.28f, 0.30f);         // 64 x 64, two teams
+    f(TileShape<1, 1, 2, 1, 3, 4>{}, 0.20f, 0.20f);         // 64 x 32, four teams
 }
 
 template <int MATS, bool BACKWARD, int ACT>
@@ -533,7 +535,7 @@ hipError_t pick(const TileParams &p, hipStream_t stream, int64_t &part_count)
 {
     float best = 0.f;
     int index = 0, chosen = -1;
-    for_shapes<MATS, BACKWARD>([&](auto shape, float alone, float in_turn) {
+    for_shapes([&](auto shape, float alone, float in_turn) {
         using S = decltype(shape);
         const int64_t tiles = (int64_t)((p.m * MATS + S::ROWS - 1) / S::ROWS) * ((p.tokens + S::TOKS - 1) / S::TOKS);
         const int64_t each = (tiles + 255) / 256;                   // tiles of the busiest CU
@@ -556,7 +558,7 @@ hipError_t pick(const TileParams &p, hipStream_t stream, int64_t &part_count)
     }
     hipError_t result = hipErrorInvalidValue;
     index = 0;
-    for_shapes<MATS, BACKWARD>([&](auto shape, float, float) {
+    for_shapes([&](auto shape, float, float) {
         if (index++ == chosen) result = go<decltype(shape), MATS, BACKWARD, ACT>(p, stream, part_count);
     });
     return result;
