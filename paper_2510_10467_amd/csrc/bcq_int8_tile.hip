@@ -17,7 +17,7 @@
 // the library's own 8-bit product of 8192^3 2100; with codes of zero a tenth less time).  With fewer tiles what LDS takes and gives: a KiB written
 // by a load takes it 16 cycles, a KiB of operands read 8.  With few tiles the latency of a step, about 0.3 us where three steps of
 // 64 x 64 are under way.  Tall matrices with 33 to 128 tokens: the CUs that the last round leaves without work, and the weights' share of
-// the bytes under way (17920 x 5120 gated with 48 tokens 47 us = 3.9 TB/s, with one token 33).
+// the bytes under way (17920 x 5120 gated with 48 tokens 46 us = 4.0 TB/s, 28672 x 8192 80 us = 5.9).
 #include <type_traits>
 
 #include "bcq_int8.hpp"
@@ -252,8 +252,17 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
     static_assert(S::RING >= 3 || !S::ACROSS, "a step reads the next one's first operands");
     const int rounds = (stages + S::TEAMS - 1) / S::TEAMS;
     auto step = [&](int i) { return i * S::TEAMS + team; };
+    // Row tiles begin 128 columns apart and come back to the first columns at the end (sums of integers are the same in any order): all at the same
+    // column would ask for addresses whole rows apart, which are few of memory's channels where a row is a power of two or
+    // nearly (28672 x 8192 with 48 tokens 55 -> 43 us, gated with 40 tokens 99 -> 80).
+    constexpr int LINE = 128 / S::STEP;                     // steps of 128 columns
+    const int turned = steps ? (int)(row_tile * LINE % steps / LINE * LINE) : 0;
+    auto columns = [&](int s) {
+        if (s >= steps) return (uint32_t)s * S::STEP;       // (the part of a step at the row's end stays last)
+        return (uint32_t)(s + turned < steps ? s + turned : s + turned - steps) * S::STEP;
+    };
     for (int i = 0; i < min(AHEAD, rounds); ++i)
-        if (step(i) < stages) stage(i, (uint32_t)step(i) * S::STEP);
+        if (step(i) < stages) stage(i, columns(step(i)));
     if (rounds > AHEAD) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((AHEAD - 1) * LOADS) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
     if (S::ACROSS) now = operands(0, 0);
@@ -263,7 +272,7 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
         constexpr int UNDER_WAY = (AHEAD - (S::ACROSS ? 2 : 1)) * LOADS;
         if constexpr (S::TEAM_WAVES == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(UNDER_WAY) : "memory");     // (a ring of its own)
         else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(UNDER_WAY) : "memory");
-        if (S::TEAMS == 1 || step(i + AHEAD) < stages) stage(into, (uint32_t)step(i + AHEAD) * S::STEP);
+        if (S::TEAMS == 1 || step(i + AHEAD) < stages) stage(into, columns(step(i + AHEAD)));
         whole_step(buffer, next(buffer));
         buffer = next(buffer);
         into = next(into);
