@@ -190,26 +190,33 @@ hipError_t go(const RowsParams &p, hipStream_t stream)
 template <int MATS>
 hipError_t pick(const RowsParams &p, hipStream_t stream)
 {
-    // More tokens' codes are worth two blocks of rows, where those still give every CU a workgroup: 14336 x 4096 with 32 tokens 13.6 -> 11.3 us
-    // (4096 x 14336 the other way, 11.4 against 15.7); 35840 x 5120 with 16 tokens 41.4 -> 36.6
-    // (with 8 tokens 34.0 both, gated 17920 x 5120 with 16 tokens the other way, 37.6 against 41.5).
-    const bool tall = p.m * MATS >= 8192;
+    // More tokens' codes are worth two blocks of rows, where those still give every CU a workgroup: 14336 x 4096 with 32 tokens 13.6 -> 11.0 us
+    // (4096 x 14336 the other way, 11.0 against 15.7); 35840 x 5120 with 16 tokens 41.4 -> 36.5 (with 8 tokens 34.0 both, gated
+    // 17920 x 5120 with 16 tokens the other way, 37.2 against 41.5).
     if (p.tokens <= 8) return go<0, MATS, 1, 4, 3>(p, stream);
     if (p.tokens <= 16) {
         if constexpr (MATS == 1)
             if (p.m >= 16384) return go<1, 1, 2, 4, 3>(p, stream);
         return go<1, MATS, 1, 4, 3>(p, stream);
     }
-    if (p.tokens <= 32) return tall ? go<2, MATS, 2, 4, 2>(p, stream) : go<2, MATS, 1, 4, 3>(p, stream);
+    if (p.tokens <= 32) {
+        if constexpr (MATS == 1)
+            if (p.m >= 8192) return go<2, 1, 2, 4, 2>(p, stream);
+        return go<2, MATS, 1, 4, 3>(p, stream);
+    }
     return go<4, MATS, 1, 4, 3>(p, stream);
 }
 
 }  // namespace
 
-// Up to 32 tokens, and up to 64 where every workgroup of 16 rows has a CU of its own (4096 x 14336 with 48 tokens 13.6 against the tiles' 16.2 us, gated
-// 4096 x 4096 8.2 against 8.5): beyond that it moves more bytes of tokens' codes than of weights, and tiles are ahead (7000 x 4096 with 48 tokens
-// 10.5 against 8.1, gated 5120 x 4096 13.4 against 10.7).
-bool int8_rows_supports(const Int8Args &a) { return a.tokens <= 32 || (a.tokens <= 64 && a.m <= 4096); }
+// Up to 16 tokens, up to 64 where every workgroup of 16 rows has a CU of its own (4096 x 14336 with 48 tokens 13.6 against the tiles' 16.2 us, gated
+// 4096 x 4096 with 24 tokens 7.3 against 8.2), and one matrix of at most 16384 rows up to 32: beyond that a workgroup moves more bytes
+// of tokens' codes than of weights, and tiles are ahead (28672 x 8192 with 24 tokens 47.1 against 42.4, with 8 tokens 40.1 against 41.9; 7000 x 4096
+// with 48 tokens 10.5 against 8.1; gated 5120 x 4096 with 24 tokens 11.0 against 9.2).
+bool int8_rows_supports(const Int8Args &a)
+{
+    return a.tokens <= 16 || (a.tokens <= 64 && a.m <= 4096) || (a.tokens <= 32 && a.matrices == 1 && a.m <= 16384);
+}
 
 hipError_t int8_rows_launch(const Int8Args &a, hipStream_t stream)
 {
