@@ -535,6 +535,9 @@ void for_shapes(F f)
     f(TileShape<2, 2, 2, 2, 4>{}, 0.60f, 0.62f);            // 128 x 128
     f(TileShape<4, 1, 2, 2, 4>{}, 0.69f, 0.70f);            // 256 x 64
     f(TileShape<2, 1, 2, 2, 6, 2, 64>{}, 0.34f, 0.50f);     // 128 x 64, two teams
+    // ... where rows are no whole lines: a piece of 64 bytes is then a line's half with one round and the other with the next (25065 x 6800 with 34
+    // tokens 50.7 -> 42.7 us, 8448 x 11680 gated with 17 65 -> 57; on whole lines 4096 x 14336 with 512 the other way, 41.7 against 47.7)
+    f(TileShape<2, 1, 2, 2, 3, 2>{}, 0.34f, 0.50f);
     f(TileShape<1, 2, 2, 1, 4, 2>{}, 0.28f, 0.30f);         // 64 x 64, two teams
     f(TileShape<1, 1, 2, 1, 3, 4>{}, 0.20f, 0.20f);         // 64 x 32, four teams
 }
@@ -542,10 +545,12 @@ void for_shapes(F f)
 template <int MATS, bool BACKWARD, int ACT>
 hipError_t pick(const TileParams &p, hipStream_t stream, int64_t &part_count)
 {
+    const bool lines = p.n % 128 == 0 && ((reinterpret_cast<uintptr_t>(p.w[0]) | reinterpret_cast<uintptr_t>(p.w[MATS - 1])) & 127) == 0;
     float best = 0.f;
     int index = 0, chosen = -1;
     for_shapes([&](auto shape, float alone, float in_turn) {
         using S = decltype(shape);
+        if (S::STEP < 128 && !lines) alone = in_turn = 1e9f;
         const int64_t tiles = (int64_t)((p.m * MATS + S::ROWS - 1) / S::ROWS) * ((p.tokens + S::TOKS - 1) / S::TOKS);
         const int64_t each = (tiles + 255) / 256;                   // tiles of the busiest CU
         const float us = each == 1 ? alone : (float)each * in_turn;
