@@ -81,7 +81,7 @@ __device__ __forceinline__ float gradient_power(float norm, float token_scale, f
 
 hipError_t int8_quantize_launch(const uint16_t *x, bool bf16, int8_t *q, float *scales, int64_t rows, int64_t n, hipStream_t stream);
 
-// Few tokens: weights stream from memory into the matrix instructions' operands, without LDS.
+// Few tokens: every wave streams rows of weights through LDS of its own.
 bool int8_rows_supports(const Int8Args &a);
 hipError_t int8_rows_launch(const Int8Args &a, hipStream_t stream);
 
