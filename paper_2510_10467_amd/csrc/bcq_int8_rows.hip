@@ -1,6 +1,6 @@
 // 8-bit products for few tokens: every wave streams rows of weights of its own through LDS of its own.
 //
-// A workgroup owns 16 BLOCKS rows (of gate and of up, where there are two) and all tokens; its waves take equal runs of 128-column steps and meet at
+// A workgroup owns 16 BLOCKS rows (of gate and of up, where there are two) and up to 16 TT tokens, mostly all; its waves take equal runs of 128-column steps and meet at
 // the end in LDS, with sums of integers, which are the same in any order.  In between they share nothing and wait for nothing but their own loads.
 //
 // v_mfma_i32_16x16x64_i8 wants 16 bytes of row lane % 16 in a lane.  Loaded like that, straight into registers, neighbouring lanes
@@ -42,8 +42,14 @@ struct RowsShape {
 };
 
 template <typename S>
-__global__ __launch_bounds__(S::WAVES * 64) void int8_rows_kernel(const RowsParams a)
+__global__ __launch_bounds__(S::WAVES * 64) void int8_rows_kernel(const RowsParams whole_call)
 {
+    RowsParams a = whole_call;                          // from here on this workgroup's tokens
+    const int t0 = (int)blockIdx.y * (S::TT * 16);
+    a.q += (int64_t)t0 * a.n;
+    a.token_scales += t0;
+    a.y += (int64_t)t0 * a.m;
+    a.tokens = min(a.tokens - t0, S::TT * 16);
     constexpr int TT = S::TT, MATS = S::MATS, BLOCKS = S::BLOCKS, WAVES = S::WAVES, RING = S::RING, WF = S::WF, FRAGS = S::FRAGS;
     constexpr int RESULTS = BLOCKS * TT * 256, EACH = (RESULTS + WAVES * 64 - 1) / (WAVES * 64);
     extern __shared__ __align__(16) unsigned char lds[];
@@ -183,8 +189,23 @@ hipError_t go(const RowsParams &p, hipStream_t stream)
     const int64_t blocks = (p.m + 16 * BLOCKS - 1) / (16 * BLOCKS);
     const auto kernel = int8_rows_kernel<S>;
     if (hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), S::BYTES)) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(WAVES * 64), S::BYTES, stream, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks, (unsigned)((p.tokens + S::TT * 16 - 1) / (S::TT * 16))), dim3(WAVES * 64), S::BYTES, stream, p);
     return hipGetLastError();
+}
+
+// The tokens of a workgroup, 0 for none: up to 16 tokens all of them.  Beyond that as few as leave every workgroup of 16 rows a CU of its own: short matrices
+// (1024 x 4096 with 100 tokens: of 16, 32, 64 tokens 4.6, 4.6, 5.8 us, tiles 6.9; 255 x 28672 with 85: 12, 16, 25, tiles 31; 4096 x 14336 with 48:
+// of 64 13.6, tiles 16.2), though with many tokens they all bring the codes again (200 x 4096 with 1000: of 64 8.4, tiles 7.3), and with
+// two matrices those of 64 only where that is all (gated 860 x 9680 with 222: 22.6, tiles 18.6).  And up to 32 tokens one matrix of at most 16384 rows
+// (14336 x 4096 with 24 tokens 10.7, tiles 11.4).  Else a workgroup moves more bytes of codes than of weights, and tiles are ahead (28672 x 8192 with
+// 24 tokens 47.1 against 42.4, with 8 tokens 40.1 against 41.9; 7000 x 4096 with 48 tokens 10.5 against 8.1).
+int tokens_of(int64_t m, int64_t tokens, int matrices)
+{
+    if (tokens <= 16) return 16;
+    if (tokens <= 256)
+        for (int some = 16; some <= 64; some *= 2)
+            if ((m + 15) / 16 * ((tokens + some - 1) / some) <= 256 && (matrices == 1 || some < 64 || tokens <= 64)) return some;
+    return tokens <= 32 && matrices == 1 && m <= 16384 ? 32 : 0;
 }
 
 template <int MATS>
@@ -193,13 +214,14 @@ hipError_t pick(const RowsParams &p, hipStream_t stream)
     // More tokens' codes are worth two blocks of rows, where those still give every CU a workgroup: 14336 x 4096 with 32 tokens 13.6 -> 11.0 us
     // (4096 x 14336 the other way, 11.0 against 15.7); 35840 x 5120 with 16 tokens 41.4 -> 36.5 (with 8 tokens 34.0 both, gated
     // 17920 x 5120 with 16 tokens the other way, 37.2 against 41.5).
+    const int some = tokens_of(p.m, p.tokens, MATS);
     if (p.tokens <= 8) return go<0, MATS, 1, 4, 3>(p, stream);
-    if (p.tokens <= 16) {
+    if (some == 16) {
         if constexpr (MATS == 1)
             if (p.m >= 16384) return go<1, 1, 2, 4, 3>(p, stream);
         return go<1, MATS, 1, 4, 3>(p, stream);
     }
-    if (p.tokens <= 32) {
+    if (some == 32) {
         if constexpr (MATS == 1)
             if (p.m >= 8192) return go<2, 1, 2, 4, 2>(p, stream);
         return go<2, MATS, 1, 4, 3>(p, stream);
@@ -209,14 +231,7 @@ hipError_t pick(const RowsParams &p, hipStream_t stream)
 
 }  // namespace
 
-// Up to 16 tokens, up to 64 where every workgroup of 16 rows has a CU of its own (4096 x 14336 with 48 tokens 13.6 against the tiles' 16.2 us, gated
-// 4096 x 4096 with 24 tokens 7.3 against 8.2), and one matrix of at most 16384 rows up to 32: beyond that a workgroup moves more bytes
-// of tokens' codes than of weights, and tiles are ahead (28672 x 8192 with 24 tokens 47.1 against 42.4, with 8 tokens 40.1 against 41.9; 7000 x 4096
-// with 48 tokens 10.5 against 8.1; gated 5120 x 4096 with 24 tokens 11.0 against 9.2).
-bool int8_rows_supports(const Int8Args &a)
-{
-    return a.tokens <= 16 || (a.tokens <= 64 && a.m <= 4096) || (a.tokens <= 32 && a.matrices == 1 && a.m <= 16384);
-}
+bool int8_rows_supports(const Int8Args &a) { return tokens_of(a.m, a.tokens, a.matrices) > 0; }
 
 hipError_t int8_rows_launch(const Int8Args &a, hipStream_t stream)
 {
