@@ -17,7 +17,7 @@
 // the library's own 8-bit product of 8192^3 2100; with codes of zero a tenth less time).  With fewer tiles what LDS takes and gives: a KiB written
 // by a load takes it 16 cycles, a KiB of operands read 8.  With few tiles the latency of a step, about 0.3 us where three steps of
 // 64 x 64 are under way.  Tall matrices with 33 to 128 tokens: the CUs that the last round leaves without work, and the weights' share of
-// the bytes under way (17920 x 5120 gated with 48 tokens 46 us = 4.0 TB/s, 28672 x 8192 80 us = 5.9).
+// the bytes under way (17920 x 5120 gated with 48 tokens 42 us = 4.4 TB/s, 28672 x 8192 80 us = 5.9).
 #include <type_traits>
 
 #include "bcq_int8.hpp"
@@ -118,7 +118,7 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
     using L = TileLds<S, MATS, BACKWARD>;
     constexpr int FRC = S::FR / MATS;                       // tiles of 32 channels in a wave
     constexpr int CHANNELS = L::CHANNELS;
-    static_assert(!BACKWARD || CHANNELS % 64 == 0 || CHANNELS == 32, "the last tile writes the gradients' rows to their end");
+    static_assert(!BACKWARD || CHANNELS % 32 == 0, "the last tile writes the gradients' rows, of a multiple of 64, to their end");
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int team = wave / S::TEAM_WAVES, tw = wave % S::TEAM_WAVES;
@@ -140,8 +140,11 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
 
     // A load brings 1 KiB: LOAD_ROWS rows; lane l delivers the part that belongs at place l % PLACES of row l / PLACES of them.
     // Rows and tokens past the end repeat the last one (their results are not stored).
-    constexpr int W_LOADS = S::ROWS / S::LOAD_ROWS / S::TEAM_WAVES, Q_LOADS = S::TOKS / S::LOAD_ROWS / S::TEAM_WAVES;
-    static_assert(W_LOADS * S::LOAD_ROWS * S::TEAM_WAVES == S::ROWS && Q_LOADS * S::LOAD_ROWS * S::TEAM_WAVES == S::TOKS, "whole loads per wave");
+    constexpr int W_LOADS = S::ROWS / S::LOAD_ROWS / S::TEAM_WAVES, Q_UNITS = S::TOKS / S::LOAD_ROWS,
+                  Q_LOADS = (Q_UNITS + S::TEAM_WAVES - 1) / S::TEAM_WAVES;
+    static_assert(W_LOADS * S::LOAD_ROWS * S::TEAM_WAVES == S::ROWS && Q_UNITS * S::LOAD_ROWS == S::TOKS, "whole loads");
+    // (six waves bring eight loads of tokens: twelve, the last ones the same)
+    auto q_unit = [&](int k) { return Q_UNITS % S::TEAM_WAVES == 0 ? tw * Q_LOADS + k : min(tw * Q_LOADS + k, Q_UNITS - 1); };
     uint32_t w_src[W_LOADS], q_src[Q_LOADS], w_part[W_LOADS], q_part[Q_LOADS];
 #pragma unroll
     for (int k = 0; k < W_LOADS; ++k) {
@@ -153,7 +156,7 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
     }
 #pragma unroll
     for (int k = 0; k < Q_LOADS; ++k) {
-        const uint32_t tok = S::LOAD_ROWS * (tw * Q_LOADS + k) + lane / S::PLACES;
+        const uint32_t tok = S::LOAD_ROWS * q_unit(k) + lane / S::PLACES;
         q_part[k] = (lane % S::PLACES ^ S::swizzle(tok)) * 16;
         q_src[k] = min(tok, toks - 1) * a.n;
     }
@@ -188,7 +191,7 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
         }
 #pragma unroll
         for (int k = 0; k < Q_LOADS; ++k) {
-            const int unit = tw * Q_LOADS + k;
+            const int unit = q_unit(k);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(q_rsrc, (__attribute__((address_space(3))) void *)(to + S::ROWS * S::STEP + unit * 1024), 16,
                                                      (int)(q_src[k] + column(q_part[k])), 0, 0, 0);
         }
@@ -460,8 +463,8 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
             if (tok < toks && ch0 + piece * 8 < a.m_padded)
                 *reinterpret_cast<u32x4 *>(a.grad + (int64_t)(t0 + tok) * a.grad_stride + k * a.m_padded + ch0 + piece * 8) =
                     *reinterpret_cast<const u32x4 *>(lds + k * L::OUT + tok * L::OUT_ROW + piece * 16);
-            if constexpr (CHANNELS < 64)                    // (its last 32 channels may be the gradients' last but 32)
-                if (tok < toks && ch0 + CHANNELS >= a.m && ch0 + CHANNELS < a.m_padded)
+            if constexpr (CHANNELS % 64 != 0)               // (the last tile may end 32 channels short of it)
+                if (piece < 4 && tok < toks && ch0 + CHANNELS >= a.m && ch0 + CHANNELS < a.m_padded)
                     *reinterpret_cast<u32x4 *>(a.grad + (int64_t)(t0 + tok) * a.grad_stride + k * a.m_padded + ch0 + CHANNELS + piece * 8) = u32x4{0, 0, 0, 0};
         }
     }
@@ -521,9 +524,12 @@ hipError_t go_mixed(TileParams p, uint32_t first_row_tiles, hipStream_t stream, 
 
 // What a workgroup takes per 128 columns, alone on its CU and as one of several in turn (microseconds, measured): the shape that is expected to be done
 // first is taken.  Large tiles read each operand from the caches the fewest times; small ones, with teams or a deep ring, give every CU work and
-// keep enough bytes under way where there are few.  (4096 columns: 4096 rows and 256 tokens 52 / 31 / 20 / 22 / 15 / 11 / 15 us from the first shape to the last,
-// 14336 rows and 512 tokens, gated, 65 / 75 / 90 / 106 / 131 / 162.  5120 columns, 17920 rows and 48 tokens, gated: 78 / 56 / 62 / 47 / 65 / 52.  4096 x 4096 with 100 tokens:
-// the last two 10.4 and 8.1.)
+// keep enough bytes under way where there are few.
+//                                       256 x 256  256 x 128  128 x 128  256 x 64  128 x 64  64 x 64  64 x 32
+//   4096 x 4096, 256 tokens                    52         31         20        22        15       11       15  us
+//   4096 x 4096, 100 tokens                    51         31         20        22        15     10.4      8.1
+//   14336 x 4096 gated, 512 tokens             65         75         90       106       131      162
+//   17920 x 5120 gated, 48 tokens              78         53         61        46        64       51       61
 using Largest = TileShape<2, 4, 4, 2, 2>;
 using Large = TileShape<4, 2, 2, 2, 3>;
 constexpr float kLargestUs = 1.70f, kLargeUs = 1.08f;
@@ -534,6 +540,8 @@ void for_shapes(F f)
     f(Large{}, kLargeUs, 1.10f);                            // 256 x 128
     f(TileShape<2, 2, 2, 2, 4>{}, 0.60f, 0.62f);            // 128 x 128
     f(TileShape<4, 1, 2, 2, 4>{}, 0.69f, 0.70f);            // 256 x 64
+    // 192 x 64: more workgroups, with more bytes under way, for heights between (17920 x 5120 gated with 48 tokens 46.2 -> 42.0 us)
+    f(TileShape<3, 2, 2, 1, 5>{}, 0.62f, 0.66f);
     f(TileShape<2, 1, 2, 2, 6, 2, 64>{}, 0.34f, 0.50f);     // 128 x 64, two teams
     // ... where rows are no whole lines: a piece of 64 bytes is then a line's half with one round and the other with the next (25065 x 6800 with 34
     // tokens 50.7 -> 42.7 us, 8448 x 11680 gated with 17 65 -> 57; on whole lines 4096 x 14336 with 512 the other way, 41.7 against 47.7)
