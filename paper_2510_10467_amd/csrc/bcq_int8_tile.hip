@@ -540,7 +540,9 @@ void for_shapes(F f)
     f(Large{}, kLargeUs, 1.10f);                            // 256 x 128
     f(TileShape<2, 2, 2, 2, 4>{}, 0.60f, 0.62f);            // 128 x 128
     f(TileShape<4, 1, 2, 2, 4>{}, 0.69f, 0.70f);            // 256 x 64
-    // 192 x 64: more workgroups, with more bytes under way, for heights between (17920 x 5120 gated with 48 tokens 46.2 -> 42.0 us)
+    // 192 x 128 and 192 x 64: more workgroups, with more bytes under way, for heights between (17920 x 5120 gated with 100 tokens 54.5 -> 49.5 us, with 48
+    // 46.2 -> 42.0; 8192 x 8192 with 600 tokens 59.9 -> 56.3)
+    f(TileShape<3, 2, 2, 2, 4>{}, 0.97f, 1.05f);
     f(TileShape<3, 2, 2, 1, 5>{}, 0.62f, 0.66f);
     f(TileShape<2, 1, 2, 2, 6, 2, 64>{}, 0.34f, 0.50f);     // 128 x 64, two teams
     // ... where rows are no whole lines: a piece of 64 bytes is then a line's half with one round and the other with the next (25065 x 6800 with 34

@@ -170,17 +170,18 @@ def test_quantize_zero_and_unfit_rows(bcq, dtype, rows):
 SIZES = [(1, 1, 16), (1, 16, 32), (2, 40, 48), (5, 17, 64), (16, 100, 112), (15, 1000, 4096), (1, 129, 1040), (3, 33, 14336),
          (17, 1, 16), (17, 40, 48), (33, 64, 128), (64, 65, 144), (77, 101, 1040), (130, 129, 80), (300, 200, 2064), (65, 1000, 272)]
 # tall and short matrices with few tokens, and each tile shape of many rows and tokens: 256 x 128, 256 x 256, 128 x 128, 128 x 64 (rows of
-# whole 128 bytes and others), 256 x 64, 192 x 64, and 256 x 256 with 256 x 128 behind them, 64 x 64, 64 x 32; short
+# whole 128 bytes and others), 256 x 64, 192 x 64, 192 x 128, and 256 x 256 with 256 x 128 behind them, 64 x 64, 64 x 32; short
 # matrices with 16, 32 and 64 tokens in a workgroup
 LARGE_SIZES = [(12, 16400, 144), (20, 8200, 272), (40, 9000, 144), (200, 16400, 144), (129, 20000, 272), (300, 33001, 208), (257, 33024, 1040),
                (500, 28600, 80), (100, 20010, 144), (100, 10001, 272), (40, 33000, 400), (64, 36001, 1040),
                (300, 48100, 80), (500, 47000, 272), (100, 20010, 256), (100, 10001, 1152),
-               (100, 8001, 272), (129, 4999, 1040), (70, 5003, 1040), (100, 1000, 272), (200, 300, 144), (150, 1200, 1040), (256, 40, 4112), (40, 50000, 272)]
+               (100, 8001, 272), (129, 4999, 1040), (70, 5003, 1040), (100, 1000, 272), (200, 300, 144), (150, 1200, 1040), (256, 40, 4112), (40, 50000, 272),
+               (100, 40000, 272), (128, 33001, 1040)]
 # ... with two matrices
 LARGE_GATED = [(20, 4100, 272), (40, 4500, 144), (200, 16400, 144), (300, 16400, 144), (200, 8200, 144), (500, 14300, 80), (100, 10010, 144), (100, 5001, 272),
                (33, 16500, 400), (50, 17001, 1040), (450, 24050, 144), (300, 23501, 80),
                (100, 10010, 256), (100, 5001, 1152), (100, 4001, 272), (70, 2500, 1040), (100, 600, 272), (200, 300, 144), (50, 25001, 400),
-               (40, 16600, 144)]
+               (40, 16600, 144), (66, 16600, 144), (100, 17000, 1040)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
