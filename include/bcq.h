@@ -273,8 +273,8 @@ int bcq_int8_gated(const int8_t *q, const float *token_scales, const int8_t *w_g
  *   workspace   at least bcq_int8_backward_workspace(matrices, m, n, tokens) bytes, 256-byte aligned, contents irrelevant before
  *               and after; matrices: 1 for bcq_int8_gemm_backward, 2 for bcq_int8_gated_backward.  Calls that may run at the same time
  *               need one each.  Fewer tokens may need more of it: ask for each number.
- * The gradients of the projections are held in 11 bits on their way into the product with the weights, scaled per token so that the ranges of dy and
- * of the activations do not matter.  Sums have a fixed order, which the sizes settle: the same call gives the same bits.
+ * The gradients of the projections times their channels' scales are held in 11 bits on their way into the product with the weights, scaled per token: each is
+ * off by up to 2^-11 of itself or 2^-25 of the token's largest, whatever the sizes of dy, of either matrix's scales and of the activations are.  Sums have a fixed order, which the sizes settle: the same call gives the same bits.
  * bcq_int8_backward_workspace returns BCQ_ERR_BAD_SHAPE for sizes that the calls refuse.  Host call.
  */
 int64_t bcq_int8_backward_workspace(int matrices, int64_t m, int64_t n, int64_t tokens);

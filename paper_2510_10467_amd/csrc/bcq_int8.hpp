@@ -66,17 +66,49 @@ __device__ __forceinline__ float activate(float g, int activation, float &slope)
     return g * s;
 }
 
-// The backward passes hold a projection's gradients G in binary16, scaled so that a token's are of the order of 1 whatever dy, the token's scale and
-// the channels' are: times `norm`, the power of two that brings the token's largest |dy| to kPlainTop (one matrix: G = dy c) or kGatedTop, and over
-// the power of two next to what the other projection is typically made of, |token_scale| top 73 73 sqrt(n) (codes spread evenly have a mean
-// square of 73^2).  It is at most 128 128 n / (73 73 sqrt(n)) = 1113 times that, so with slopes of at most 1.13 a scaled G stays below
-// 2 kGatedTop 2 1113 1.13 = 40300: nothing overflows that has a number for its gradient.
-constexpr int kPlainTop = 9, kGatedTop = 3;             // exponents
-__device__ __forceinline__ float gradient_power(float norm, float token_scale, float top, float typical)
+// The backward passes hold the projections' gradients times their channels' scales, G, in binary16 between their two products, times a power of two for
+// each token: what lies above 2^-14 has 11 bits then, what lies below is off by up to 2^-25.
+// One matrix: G = dy c, and the power brings a token's largest to 2^14.
+// Two: dg c_gate and du c_up are both at most 1.13 dh c_gate c_up |s| |sum q w|, of which |sum q w| <= |q| 128 sqrt(n) (|act(g)| <= |g|, |act'| <= 1.13).  The
+// power brings the largest such product of the token to between 2^13 and 2^15, so that nothing overflows that has a number for its
+// gradient.  What the token's largest really is depends on the weights' codes and on the activation: 2^5 and more where
+// those are as usual.  Where it ends below 1 (gates that are all shut, say), the token's gradients are made a second time, with the power that fits.  So
+// a gradient is off by up to 2^-11 of itself or 2^-25 of its token's largest.
+constexpr int kTop = 14, kGatedTop = 13;                // exponents
+constexpr int kMostPower = 126;                         // of a power, either way
+constexpr float kFitsFrom = 1.f, kFitsTo = 65000.f;
+// Whether a token's first power fits, by its largest G: `some`, there is one between kFitsFrom and kFitsTo; `other`, the largest that is not, as fp32's
+// bits.  (Above kFitsTo: only where the scales' product leaves fp32.)
+struct TokenFit {
+    uint32_t *some, *other;
+};
+__device__ __forceinline__ bool power_fits(const TokenFit &fit, int64_t token)
 {
-    const float size = fabsf(token_scale) * top * typical;              // (typical: 73 73 sqrt(n), or 0 for one matrix)
-    if (!(size > 0.f && size < __builtin_inff())) return norm;
-    return ldexpf(1.f, min(max(ilogbf(norm) - ilogbf(size), -120), 120));
+    const uint32_t some = fit.some[token];              // (both loads at once)
+    const float other = __builtin_bit_cast(float, fit.other[token]);
+    return (other == 0.f) | (other == __builtin_inff()) | ((some != 0) & (other <= kFitsTo));
+}
+__device__ __forceinline__ float token_power(const float *first, const TokenFit &fit, int64_t token)
+{
+    if (power_fits(fit, token)) return first[token];
+    const int e = ilogbf(first[token]) + kTop - ilogbf(__builtin_bit_cast(float, fit.other[token]));
+    return ldexpf(1.f, min(max(e, -kMostPower), kMostPower));
+}
+
+// The gradients of the channels' scales: a channel's partial sums in order, eight under way at a time.  parts: [count][channels]
+__device__ __forceinline__ float sum_of_parts(const float *parts, int64_t count, int64_t channels, int64_t channel)
+{
+    float sum = 0.f;
+    int64_t p = 0;
+    for (; p + 8 <= count; p += 8) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = parts[(p + k) * channels + channel];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += v[k];
+    }
+    for (; p < count; ++p) sum += parts[p * channels + channel];
+    return sum;
 }
 
 hipError_t int8_quantize_launch(const uint16_t *x, bool bf16, int8_t *q, float *scales, int64_t rows, int64_t n, hipStream_t stream);
@@ -93,13 +125,13 @@ struct Int8Workspace {
     int64_t grad_stride;            // halves between tokens: matrices * m rounded up to 64
     int splits;                     // runs of channels whose contributions to dx are summed apart
     int second_shape;               // ... and the tiles that they are taken in
-    int64_t grad, norms, scale_top, parts, split_sums, bytes;       // offsets in bytes, and the whole
+    int64_t grad, powers, some, other, parts, split_sums, bytes;    // offsets in bytes, and the whole
     int64_t part_count;             // room for so many partial sums of a channel
-    float typical;                  // what gradient_power counts with
 };
 Int8Workspace int8_workspace(int matrices, int64_t m, int64_t n, int64_t tokens);
-// the gradients of the projections, scaled as int8_backward_* explains, and partial sums of the channel scales' gradients
-hipError_t int8_tile_backward_launch(const Int8Args &a, const Int8Workspace &ws, hipStream_t stream, int64_t &part_count);
+// The gradients of the projections and partial sums of the channel scales' gradients.  again (two matrices): the gradients of the tokens whose power did not
+// fit, and with add_up the partial sums' sums.
+hipError_t int8_tile_backward_launch(const Int8Args &a, const Int8Workspace &ws, bool again, bool add_up, hipStream_t stream, int64_t &part_count);
 hipError_t int8_backward_launch(const Int8Args &a, hipStream_t stream);
 
 }  // namespace bcq

@@ -1,9 +1,9 @@
 // The backward passes of the 8-bit products, codes fixed: gradients of the activations and of the channel scales.
 //
-//   norms     per token the power of two that brings its largest |dy| to a fixed size, and the power of two above all channel scales, S
-//   first     (bcq_int8_tile.hip) G = binary16 of f_t dg c / S for every channel of every matrix, and partial sums of dc; f_t: a power of two made of
-//             the token's norm and scale and S, which brings its G near 1 (gradient_power)
-//   second    dx = (S / f_t) sum over channels of G w: a product over the weights' ROWS
+//   powers    per token the power of two, f_t, that brings its gradients to where binary16 holds them best, as far as that is known beforehand
+//   first     (bcq_int8_tile.hip) G = binary16 of f_t dg c for every channel of every matrix, the largest of each token, and partial sums of dc
+//   again     two matrices: G once more, by the largest, of tiles with tokens whose f_t did not fit; hardly ever more than a look
+//   second    dx = (1 / f_t) sum over channels of G w: a product over the weights' ROWS
 //   finish    dc: the partial sums of a channel, in order; dx where the channels were taken in several runs: the runs' sums, in order
 //
 // The second product runs on v_mfma_f32_32x32x16_f16.  Both operands go into LDS by loads that write there, the weights as they are stored: 64
@@ -13,8 +13,9 @@
 //
 // What bounds it: the power of the matrix pipe on random operands (2048 tokens, 4096 columns, 2 x 14336 channels: 437 to 459 us = 1100 to 1050 TFLOP/s,
 // with gradients of zero 330; the library's plain binary16 product of 8192^3 1300), the codes' conversion beside it, and with few tokens
-// the weights' bytes (17920 x 5120, gated, 48 tokens: 47 us = 3.9 TB/s).  The whole gated backward pass of 2048 tokens: 700 us, of which the
-// norms 13, the first half 290, the finish 5.
+// the weights' bytes (17920 x 5120, gated, 48 tokens: 47 us = 3.9 TB/s).  The whole gated backward pass of 2048 tokens: 729 us; the
+// profiler, which counts the time that two launches overlap twice, has 18 for the powers, 295 for the first half, 5 for the second look with the sums, 447
+// for the second half.
 #include <math.h>
 
 #include "bcq_int8.hpp"
@@ -28,59 +29,114 @@ typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef int v2i __attribute__((ext_vector_type(2)));
 
-// One workgroup per token, and a first one for the scales.  Four loads of a thread are under way at a time.
-__global__ __launch_bounds__(256) void int8_norms_kernel(const uint16_t *__restrict__ dy, const float *__restrict__ c0, const float *__restrict__ c1,
-                                                         float *__restrict__ norms, float *__restrict__ scale_top, int64_t m, int exponent, bool bf16,
-                                                         bool whole)
+// A token's power of two from the largest |dy c| of its channels, or, where there are two matrices, |dh c_gate c_up| and its codes' length.  A workgroup takes TOKENS of
+// them, which share the channels' scales on their way (2048 tokens, 14336 channels: one each 24 us, four 18).
+template <int TOKENS, int MATS>
+__global__ __launch_bounds__(256) void int8_powers_kernel(const uint16_t *__restrict__ dy, const float *__restrict__ c0, const float *__restrict__ c1,
+                                                          const int8_t *__restrict__ q, const float *__restrict__ token_scales,
+                                                          float *__restrict__ powers, const TokenFit fit, int64_t m, int64_t n, int64_t tokens, bool bf16,
+                                                          bool whole)
 {
-    __shared__ float tops[4];
-    float top = 0.f;                                    // (a NaN leaves it as it is: such a token's results are NaN whatever its power)
-    const bool for_scales = blockIdx.x == 0;
-    const int64_t token = (int64_t)blockIdx.x - 1;
+    __shared__ float tops[TOKENS][4];
+    __shared__ int squares[TOKENS][4];
+    const int64_t token0 = (int64_t)blockIdx.x * TOKENS;
     const int last = (int)m - 1;                        // what lies past the end counts the last value again
-    if (for_scales) {
-        for (int j = threadIdx.x; j <= last; j += 2048) {
-            float v[8], u[8];
+    const uint16_t *row[TOKENS];
+    float top[TOKENS];                                  // (a NaN leaves it as it is: such a token's results are NaN whatever its power)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                v[k] = c0[min(j + k * 256, last)];
-                u[k] = c1[min(j + k * 256, last)];
+    for (int t = 0; t < TOKENS; ++t) {
+        row[t] = dy + min(token0 + t, tokens - 1) * m;
+        top[t] = 0.f;
+    }
+    auto take = [&](int t, uint32_t bits, float a, float b) {
+        float v = fabsf(from_16(bits, bf16)) * fabsf(a);
+        if constexpr (MATS == 2) v *= fabsf(b);
+        top[t] = fmaxf(top[t], v);
+    };
+    v4i code[TOKENS];                                   // (asked for before what follows)
+    if constexpr (MATS == 2)
+#pragma unroll
+        for (int t = 0; t < TOKENS; ++t) code[t] = reinterpret_cast<const v4i *>(q + min(token0 + t, tokens - 1) * n)[min((int)threadIdx.x, (int)(n / 16) - 1)];
+    constexpr int AT_ONCE = TOKENS == 1 ? 2 : 1;
+    if (whole) {
+        const int last_piece = (int)(m / 8) - 1;
+        for (int j = threadIdx.x; j <= last_piece; j += AT_ONCE * 256) {
+            u32x4 v[AT_ONCE][TOKENS];
+            v4f a[AT_ONCE][2], b[AT_ONCE][2];
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const int piece = min(j + k * 256, last_piece);
+#pragma unroll
+                for (int t = 0; t < TOKENS; ++t) v[k][t] = reinterpret_cast<const u32x4 *>(row[t])[piece];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    a[k][h] = reinterpret_cast<const v4f *>(c0)[2 * piece + h];
+                    b[k][h] = MATS == 2 ? reinterpret_cast<const v4f *>(c1)[2 * piece + h] : a[k][h];
+                }
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) top = fmaxf(top, fmaxf(fabsf(v[k]), fabsf(u[k])));
-        }
-    } else if (whole) {
-        const u32x4 *row = reinterpret_cast<const u32x4 *>(dy + token * m);
-        const int last_piece = (int)(m / 8) - 1;
-        for (int j = threadIdx.x; j <= last_piece; j += 1024) {
-            u32x4 v[4];
+            for (int k = 0; k < AT_ONCE; ++k)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = row[min(j + k * 256, last_piece)];
+                for (int t = 0; t < TOKENS; ++t)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        take(t, (i & 1) ? v[k][t][i >> 1] >> 16 : v[k][t][i >> 1] & 0xffffu, a[k][i >> 2][i & 3], b[k][i >> 2][i & 3]);
+        }
+    } else {
+        for (int j = threadIdx.x; j <= last; j += 1024) {
+            uint32_t v[4][TOKENS];
+            float a[4], b[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int at = min(j + k * 256, last);
+                a[k] = c0[at];
+                b[k] = MATS == 2 ? c1[at] : 0.f;
+#pragma unroll
+                for (int t = 0; t < TOKENS; ++t) v[k][t] = row[t][at];
+            }
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(from_16(v[k][i] & 0xffffu, bf16)), fabsf(from_16(v[k][i] >> 16, bf16))));
-        }
-    } else {
-        const uint16_t *row = dy + token * m;
-        for (int j = threadIdx.x; j <= last; j += 1024) {
-            uint32_t v[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = row[min(j + k * 256, last)];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) top = fmaxf(top, fabsf(from_16(v[k], bf16)));
+                for (int t = 0; t < TOKENS; ++t) take(t, v[k][t], a[k], b[k]);
         }
     }
+    int square[TOKENS];                                 // (131056 squares of 128 stay below 2^31)
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
-    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    for (int t = 0; t < TOKENS; ++t) square[t] = 0;
+    if constexpr (MATS == 2)
+        for (int j = threadIdx.x; j < (int)(n / 16); j += 256)
+#pragma unroll
+            for (int t = 0; t < TOKENS; ++t) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) square[t] = __builtin_amdgcn_sdot4(code[t][i], code[t][i], square[t], false);
+                if (j + 256 < (int)(n / 16)) code[t] = reinterpret_cast<const v4i *>(q + min(token0 + t, tokens - 1) * n)[j + 256];
+            }
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t) {
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            top[t] = fmaxf(top[t], __shfl_xor(top[t], d, 64));
+            if constexpr (MATS == 2) square[t] += __shfl_xor(square[t], d, 64);
+        }
+        if ((threadIdx.x & 63) == 0) {
+            tops[t][threadIdx.x >> 6] = top[t];
+            squares[t][threadIdx.x >> 6] = square[t];
+        }
+    }
     __syncthreads();
-    if (threadIdx.x != 0) return;
-    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    const bool usable = top > 0.f && top < __builtin_inff();
-    const int e = usable ? min(max(ilogbf(top), -110), 110) : 0;
-    if (for_scales) *scale_top = ldexpf(1.f, usable ? e + 1 : 0);
-    else norms[token] = ldexpf(1.f, usable ? exponent - e : 0);
+    const int t = threadIdx.x;
+    if (t >= TOKENS || token0 + t >= tokens) return;
+    auto usable = [](float v) { return v > 0.f && v < __builtin_inff(); };
+    const float most = fmaxf(fmaxf(tops[t][0], tops[t][1]), fmaxf(tops[t][2], tops[t][3]));
+    int e = MATS == 2 ? kGatedTop : kTop;
+    if (usable(most)) e -= ilogbf(most);
+    if constexpr (MATS == 2) {
+        const float length = sqrtf((float)(squares[t][0] + squares[t][1] + squares[t][2] + squares[t][3]));
+        const float sums = fabsf(token_scales[token0 + t]) * (1.13f * 128.f * sqrtf((float)n) * length);
+        if (usable(sums)) e -= ilogbf(sums);
+        fit.some[token0 + t] = fit.other[token0 + t] = 0;
+    }
+    powers[token0 + t] = ldexpf(1.f, min(max(e, -kMostPower), kMostPower));
 }
 
 constexpr uint32_t kTokenGroup = 4;       // token tiles whose workgroups run beside each other for a column tile
@@ -88,8 +144,8 @@ constexpr uint32_t kTokenGroup = 4;       // token tiles whose workgroups run be
 struct SecondParams {
     const _Float16 *grad;
     const int8_t *w[2];
-    const float *norms, *token_scales, *scale_top;
-    float typical;
+    const float *powers;
+    TokenFit fit;
     uint16_t *dx;
     uint32_t m, m_padded, n, tokens, grad_stride;
     uint32_t column_tiles, token_tiles;
@@ -321,12 +377,11 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_second_kernel(const Sec
         }
         return;
     }
-    const float top = *a.scale_top;
 #pragma unroll
     for (int t = 0; t < (team == 0 ? S::FT : 0); ++t) {
         const uint32_t tok = (wt * S::FT + t) * 32 + r32;
         const uint32_t at = t0 + min(tok, toks - 1);
-        const float back = top / gradient_power(a.norms[at], a.token_scales[at], top, a.typical);       // (powers of two)
+        const float back = 1.f / (a.matrices == 2 ? token_power(a.powers, a.fit, at) : a.powers[at]);     // (powers of two)
 #pragma unroll
         for (int c = 0; c < S::FC; ++c)
 #pragma unroll
@@ -347,11 +402,11 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_second_kernel(const Sec
     }
 }
 
-// What is left, in one launch: the first sums_blocks workgroups add up the partial sums of the scales' gradients, in order, a channel a thread and eight
-// under way at a time; the others the runs' sums of dx, four columns a thread.
+// What is left, in one launch: the first sums_blocks workgroups add up the partial sums of the scales' gradients, a channel a thread; the
+// others the runs' sums of dx, four columns a thread.
 struct FinishParams {
-    const float *parts, *split_sums, *norms, *token_scales, *scale_top;
-    float typical;
+    const float *parts, *split_sums, *powers;
+    TokenFit fit;
     float *dscales[2];
     uint16_t *dx;
     int64_t m, part_count, tokens;
@@ -363,18 +418,9 @@ struct FinishParams {
 __global__ __launch_bounds__(64) void int8_finish_kernel(const FinishParams a)
 {
     if (blockIdx.x < a.sums_blocks) {
-        const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x, stride = a.m * a.matrices;
-        if (i >= stride) return;
-        float sum = 0.f;
-        int64_t p = 0;
-        for (; p + 8 <= a.part_count; p += 8) {
-            float v[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = a.parts[(p + k) * stride + i];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sum += v[k];
-        }
-        for (; p < a.part_count; ++p) sum += a.parts[p * stride + i];
+        const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x, channels = a.m * a.matrices;
+        if (i >= channels) return;
+        const float sum = sum_of_parts(a.parts, a.part_count, channels, i);
         if (i < a.m) a.dscales[0][i] = sum;
         else a.dscales[1][i - a.m] = sum;
         return;
@@ -385,7 +431,7 @@ __global__ __launch_bounds__(64) void int8_finish_kernel(const FinishParams a)
 #pragma unroll 4
     for (int s = 0; s < a.splits; ++s) sum += reinterpret_cast<const v4f *>(a.split_sums)[s * count + i];
     const int64_t token = i * 4 / a.n;
-    const float top = *a.scale_top, back = top / gradient_power(a.norms[token], a.token_scales[token], top, a.typical);     // (powers of two)
+    const float back = 1.f / (a.matrices == 2 ? token_power(a.powers, a.fit, token) : a.powers[token]);     // (powers of two)
     uint32_t out[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) out[k] = to_16(sum[k] * back, a.bf16);
@@ -445,6 +491,22 @@ SecondPlan second_plan(int matrices, int64_t m, int64_t n, int64_t tokens)
     return plan;
 }
 
+template <int TOKENS, int MATS>
+hipError_t powers_go(const Int8Args &a, float *powers, const TokenFit &fit, hipStream_t stream)
+{
+    const float *c0 = a.channel_scales[0], *c1 = a.channel_scales[MATS - 1];
+    const bool whole = a.m % 8 == 0 && ((reinterpret_cast<uintptr_t>(a.dy) | reinterpret_cast<uintptr_t>(c0) | reinterpret_cast<uintptr_t>(c1)) & 15) == 0;
+    hipLaunchKernelGGL((int8_powers_kernel<TOKENS, MATS>), dim3((unsigned)((a.tokens + TOKENS - 1) / TOKENS)), dim3(256), 0, stream, a.dy, c0, c1, a.q,
+                       a.token_scales, powers, fit, a.m, a.n, a.tokens, a.bf16, whole);
+    return hipGetLastError();
+}
+
+hipError_t powers_launch(const Int8Args &a, float *powers, const TokenFit &fit, hipStream_t stream)
+{
+    if (a.tokens >= 1024) return a.matrices == 2 ? powers_go<4, 2>(a, powers, fit, stream) : powers_go<4, 1>(a, powers, fit, stream);
+    return a.matrices == 2 ? powers_go<1, 2>(a, powers, fit, stream) : powers_go<1, 1>(a, powers, fit, stream);
+}
+
 }  // namespace
 
 Int8Workspace int8_workspace(int matrices, int64_t m, int64_t n, int64_t tokens)
@@ -456,11 +518,11 @@ Int8Workspace int8_workspace(int matrices, int64_t m, int64_t n, int64_t tokens)
     const SecondPlan plan = second_plan(matrices, m, n, tokens);
     ws.second_shape = plan.shape;
     ws.splits = plan.splits;
-    ws.typical = matrices == 1 ? 0.f : 73.f * 73.f * sqrtf((float)n);
     ws.grad = 0;
-    ws.norms = up(tokens * ws.grad_stride * 2);
-    ws.scale_top = ws.norms + up(tokens * 4);
-    ws.parts = ws.scale_top + 256;
+    ws.powers = up(tokens * ws.grad_stride * 2);
+    ws.some = ws.powers + up(tokens * 4);
+    ws.other = ws.some + (matrices == 2 ? up(tokens * 4) : 0);
+    ws.parts = ws.other + (matrices == 2 ? up(tokens * 4) : 0);
     ws.split_sums = ws.parts + up(ws.part_count * matrices * m * 4);
     ws.bytes = ws.split_sums + (ws.splits > 1 ? up(ws.splits * tokens * n * 4) : 0);
     return ws;
@@ -470,39 +532,22 @@ hipError_t int8_backward_launch(const Int8Args &a, hipStream_t stream)
 {
     const Int8Workspace ws = int8_workspace(a.matrices, a.m, a.n, a.tokens);
     unsigned char *base = static_cast<unsigned char *>(a.workspace);
-    float *norms = reinterpret_cast<float *>(base + ws.norms), *scale_top = reinterpret_cast<float *>(base + ws.scale_top);
-    FinishParams f{};
-    f.parts = reinterpret_cast<const float *>(base + ws.parts);
-    f.split_sums = reinterpret_cast<const float *>(base + ws.split_sums);
-    f.norms = norms;
-    f.token_scales = a.token_scales;
-    f.typical = ws.typical;
-    f.scale_top = scale_top;
-    f.dscales[0] = a.dscales[0];
-    f.dscales[1] = a.dscales[a.matrices - 1];
-    f.dx = a.dx;
-    f.m = a.m;
-    f.tokens = a.tokens;
-    f.n = (uint32_t)a.n;
-    f.sums_blocks = (uint32_t)((a.m * a.matrices + 63) / 64);
-    f.matrices = a.matrices;
-    f.splits = ws.splits;
-    f.bf16 = a.bf16;
+    float *powers = reinterpret_cast<float *>(base + ws.powers), *split_sums = reinterpret_cast<float *>(base + ws.split_sums);
+    const TokenFit fit = {reinterpret_cast<uint32_t *>(base + ws.some), reinterpret_cast<uint32_t *>(base + ws.other)};
+    // The scales' gradients are added up in the launch that adds up the runs of dx, or, where there is none and two matrices, in the second look at the gradients.
+    const bool runs = ws.splits > 1 && a.tokens > 0, finish = runs || a.matrices == 1 || a.tokens == 0;
+    int64_t part_count = 0;
     if (a.tokens > 0) {
-        const bool whole = a.m % 8 == 0 && (reinterpret_cast<uintptr_t>(a.dy) & 15) == 0;
-        hipLaunchKernelGGL(int8_norms_kernel, dim3((unsigned)(a.tokens + 1)), dim3(256), 0, stream, a.dy, a.channel_scales[0],
-                           a.channel_scales[a.matrices - 1], norms, scale_top, a.m,
-                           a.matrices == 1 ? kPlainTop : kGatedTop, a.bf16, whole);
-        if (hipError_t e = hipGetLastError()) return e;
-        if (hipError_t e = int8_tile_backward_launch(a, ws, stream, f.part_count)) return e;
+        if (hipError_t e = powers_launch(a, powers, fit, stream)) return e;
+        if (hipError_t e = int8_tile_backward_launch(a, ws, false, false, stream, part_count)) return e;
+        if (a.matrices == 2)
+            if (hipError_t e = int8_tile_backward_launch(a, ws, true, !finish, stream, part_count)) return e;
         SecondParams p{};
         p.grad = reinterpret_cast<const _Float16 *>(base + ws.grad);
         p.w[0] = a.w[0];
         p.w[1] = a.w[a.matrices - 1];
-        p.norms = norms;
-        p.token_scales = a.token_scales;
-        p.typical = ws.typical;
-        p.scale_top = scale_top;
+        p.powers = powers;
+        p.fit = fit;
         p.dx = a.dx;
         p.m = (uint32_t)a.m;
         p.m_padded = (uint32_t)(ws.grad_stride / a.matrices);
@@ -512,7 +557,7 @@ hipError_t int8_backward_launch(const Int8Args &a, hipStream_t stream)
         p.matrices = a.matrices;
         p.bf16 = a.bf16;
         p.splits = ws.splits;
-        p.split_sums = reinterpret_cast<float *>(base + ws.split_sums);
+        p.split_sums = split_sums;
         hipError_t result = hipErrorInvalidValue;
         int index = 0;
         for_shapes([&](auto shape, float, float) {
@@ -520,7 +565,24 @@ hipError_t int8_backward_launch(const Int8Args &a, hipStream_t stream)
         });
         if (result) return result;
     }
-    const int64_t split_blocks = ws.splits > 1 ? (a.tokens * a.n / 4 + 63) / 64 : 0;
+    if (!finish) return hipSuccess;
+    FinishParams f{};
+    f.parts = reinterpret_cast<const float *>(base + ws.parts);
+    f.split_sums = split_sums;
+    f.powers = powers;
+    f.fit = fit;
+    f.dscales[0] = a.dscales[0];
+    f.dscales[1] = a.dscales[a.matrices - 1];
+    f.dx = a.dx;
+    f.m = a.m;
+    f.part_count = part_count;
+    f.tokens = a.tokens;
+    f.n = (uint32_t)a.n;
+    f.sums_blocks = (uint32_t)((a.m * a.matrices + 63) / 64);
+    f.matrices = a.matrices;
+    f.splits = ws.splits;
+    f.bf16 = a.bf16;
+    const int64_t split_blocks = runs ? (a.tokens * a.n / 4 + 63) / 64 : 0;
     hipLaunchKernelGGL(int8_finish_kernel, dim3((unsigned)(f.sums_blocks + split_blocks)), dim3(64), 0, stream, f);
     return hipGetLastError();
 }

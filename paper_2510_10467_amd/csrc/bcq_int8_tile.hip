@@ -41,8 +41,11 @@ struct TileParams {
     bool bf16, whole;               // whole: rows of y and dy are in pieces of 16 bytes
     // backward
     const uint16_t *dy;
-    const float *norms, *scale_top;
-    float typical;
+    const float *powers;
+    TokenFit fit;                   // two matrices
+    bool again, add_up;             // ... only tiles with tokens whose power does not fit; and the sums of `parts`
+    float *dscales[2];
+    uint32_t part_count, sums_blocks;
     _Float16 *grad;                 // [tokens][grad_stride]: matrix k from k * m_padded on
     uint32_t grad_stride, m_padded;
     float *parts;                   // [a wave's tokens, from the first on][matrices][m]
@@ -135,6 +138,14 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
     const uint32_t ch0 = part.first_channel + row_tile * CHANNELS, t0 = token_tile * S::TOKS;
 
     const uint32_t chs = min((uint32_t)CHANNELS, a.m - ch0), toks = min((uint32_t)S::TOKS, a.tokens - t0);
+    if constexpr (BACKWARD && MATS == 2) {
+        if (a.again) {                                      // (every wave looks at all of them and comes to the same answer)
+            bool all_fit = true;
+#pragma unroll
+            for (int k = 0; k < S::TOKS; k += 64) all_fit &= power_fits(a.fit, t0 + min((uint32_t)(k + lane), toks - 1));
+            if (__all(all_fit)) return;
+        }
+    }
     const int8_t *const q_base = a.q + (int64_t)t0 * a.n;
     const int8_t *const w_base = a.w[0] + (int64_t)ch0 * a.n, *const u_base = a.w[MATS - 1] + (int64_t)ch0 * a.n;
 
@@ -336,10 +347,10 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
         scales[i] = ch < chs ? a.channel_scales[i / CHANNELS][ch0 + ch] : 0.f;
     }
     float *token_scales = reinterpret_cast<float *>(lds + L::TOKEN_SCALES);
-    [[maybe_unused]] float *norms = token_scales + S::TOKS;
+    [[maybe_unused]] float *powers = token_scales + S::TOKS;
     for (uint32_t i = threadIdx.x; i < S::TOKS; i += S::WAVES * 64) {
         token_scales[i] = i < toks ? a.token_scales[t0 + i] : 0.f;
-        if constexpr (BACKWARD) norms[i] = i < toks ? gradient_power(a.norms[t0 + i], token_scales[i], *a.scale_top, a.typical) : 1.f;
+        if constexpr (BACKWARD) powers[i] = i >= toks ? 1.f : MATS == 2 && a.again ? token_power(a.powers, a.fit, t0 + i) : a.powers[t0 + i];
     }
     if constexpr (BACKWARD) {
         if (a.whole) {
@@ -365,8 +376,9 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
     }
     __syncthreads();
 
-    [[maybe_unused]] float inv_top = 0.f;
-    if constexpr (BACKWARD) inv_top = 1.f / *a.scale_top;   // (a power of two)
+    [[maybe_unused]] float largest[S::FT];
+#pragma unroll
+    for (int t = 0; t < S::FT; ++t) largest[t] = 0.f;
     // 32 sums over this wave's tokens at a time: a tile of channels of each matrix, or two tiles of the one
     constexpr int TOGETHER = BACKWARD && MATS == 1 ? 2 : 1;
     static_assert(FRC % TOGETHER == 0, "whole exchanges");
@@ -383,8 +395,8 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
                 for (int t = 0; t < S::FT; ++t) {
                     const uint32_t tok = (wt * S::FT + t) * 32 + r32;
                     const float ts = token_scales[tok];
-                    [[maybe_unused]] float norm = 0.f;
-                    if constexpr (BACKWARD) norm = norms[tok];
+                    [[maybe_unused]] float power = 0.f;
+                    if constexpr (BACKWARD) power = powers[tok];
 #pragma unroll
                     for (int e = 0; e < GROUPS; ++e) {
                         const int ch = (wr * FRC + r) * 32 + 8 * (team * GROUPS + e) + 4 * half;    // element i: channel ch + i
@@ -406,18 +418,18 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
                             } else {
                                 // (channels and tokens past the end have a gradient and a scale of 0)
                                 const float d = from_16((i & 1) ? dy[i >> 1] >> 16 : dy[i >> 1] & 0xffffu, a.bf16);
-                                // The gradients that the second half multiplies are held in binary16 (11 bits): times the token's power of
-                                // two (gradient_power) and the channel's scale over the power of two above all scales.  A value is off by 2^-12
-                                // of itself, as much as by a result's last rounding, or by 2^-25 of what is of the order of the
-                                // token's largest.
+                                // What the second half multiplies is held in binary16, times the token's power of two: off by up to
+                                // 2^-11 of itself, as much as by a binary16 result's last rounding, or by 2^-25 of the token's largest.
                                 if constexpr (MATS == 1) {
-                                    out[i] = to_16(d * (norm * (c0[i] * inv_top)), false);
+                                    out[i] = to_16(d * c0[i] * power, false);
                                     sums[(r - r0) * 16 + 4 * e + i] += d * p;
                                 } else {
                                     const float act = activate<true>(p * c0[i], ACT, slope);
                                     const float dg = d * (p2 * c1[i]) * slope, du = d * act;
-                                    out[i] = to_16(dg * (norm * (c0[i] * inv_top)), false);
-                                    out2[i] = to_16(du * (norm * (c1[i] * inv_top)), false);
+                                    const float held = dg * c0[i] * power, held2 = du * c1[i] * power;
+                                    out[i] = to_16(held, false);
+                                    out2[i] = to_16(held2, false);
+                                    largest[t] = fmaxf(largest[t], fmaxf(fabsf(held), fabsf(held2)));      // (a NaN leaves it as it is)
                                     sums[4 * e + i] += dg * p;
                                     sums[16 + 4 * e + i] += du * p2;
                                 }
@@ -426,7 +438,9 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
                         *reinterpret_cast<u32x2 *>(at) = u32x2{out[0] | out[1] << 16, out[2] | out[3] << 16};
                         if constexpr (BACKWARD && MATS == 2)
                             *reinterpret_cast<u32x2 *>(at + L::OUT) = u32x2{out2[0] | out2[1] << 16, out2[2] | out2[3] << 16};
-                        if constexpr (BACKWARD) __builtin_amdgcn_sched_barrier(0);      // (four elements at a time: registers)
+                        // (four elements at a time: registers.  A maximum put off would hold all that it is taken of.)
+                        if constexpr (BACKWARD && MATS == 2) asm volatile("" : "+v"(largest[t]));
+                        if constexpr (BACKWARD) __builtin_amdgcn_sched_barrier(0);
                     }
                 }
             if constexpr (BACKWARD) {
@@ -435,11 +449,25 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
                 const int second = r32 >> 4, e = (r32 >> 2) & 3, i = r32 & 3;
                 const uint32_t ch = (wr * FRC + r0 + (MATS == 1 ? second : 0)) * 32 + 8 * (team * GROUPS + e) + 4 * half + i;
                 float *parts = a.parts + (int64_t)(token_tile * S::WT + wt) * MATS * a.m;
-                if (e < GROUPS && ch < chs) parts[(int64_t)(MATS == 1 ? 0 : second) * a.m + ch0 + ch] = sum;
+                if (e < GROUPS && ch < chs && !(MATS == 2 && a.again)) parts[(int64_t)(MATS == 1 ? 0 : second) * a.m + ch0 + ch] = sum;
             }
         }
     };
     results();
+    if constexpr (BACKWARD && MATS == 2) {
+        if (!a.again) {
+#pragma unroll
+            for (int t = 0; t < S::FT; ++t) {
+                const float v = fmaxf(largest[t], __shfl_xor(largest[t], 32, 64));
+                const uint32_t tok = (wt * S::FT + t) * 32 + r32;
+                if (half == 1 || tok >= toks) continue;
+                // (mostly a store, of the same value by all; maxima of all tiles at once took 14336 channels with 64 tokens 12 us.  They are the
+                // same in any order.)
+                if (v >= kFitsFrom && v <= kFitsTo) a.fit.some[t0 + tok] = 1;
+                else if (v > 0.f) atomicMax(a.fit.other + t0 + tok, __builtin_bit_cast(uint32_t, v));
+            }
+        }
+    }
     __syncthreads();
 
     if constexpr (!BACKWARD) {
@@ -470,10 +498,31 @@ __device__ __forceinline__ void tile(const TileParams &a, const TilePart &part, 
     }
 }
 
+// A launch's first workgroups may add up the partial sums, a channel a thread.  Returns which of the tiles' workgroups this one is, or
+// none of them (negative).
+template <typename S, int MATS, bool BACKWARD>
+__device__ __forceinline__ int tile_of_launch(const TileParams &a)
+{
+    if constexpr (BACKWARD && MATS == 2) {
+        if (blockIdx.x < a.sums_blocks) {
+            const uint32_t i = blockIdx.x * (S::WAVES * 64) + threadIdx.x, channels = 2 * a.m;
+            if (i >= channels) return -1;
+            const float sum = sum_of_parts(a.parts, a.part_count, channels, i);
+            if (i < a.m) a.dscales[0][i] = sum;
+            else a.dscales[1][i - a.m] = sum;
+            return -1;
+        }
+        return (int)(blockIdx.x - a.sums_blocks);
+    }
+    return (int)blockIdx.x;
+}
+
 template <typename S, int MATS, bool BACKWARD, int ACT>
 __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_tile_kernel(const TileParams a)
 {
-    tile<S, MATS, BACKWARD, ACT>(a, a.part[0], blockIdx.x);
+    const int block = tile_of_launch<S, MATS, BACKWARD>(a);
+    if (block < 0) return;
+    tile<S, MATS, BACKWARD, ACT>(a, a.part[0], (uint32_t)block);
 }
 
 // Two shapes in one launch: the second's workgroups are behind the first's.
@@ -481,16 +530,18 @@ template <typename S, typename S2, int MATS, bool BACKWARD, int ACT>
 __global__ __launch_bounds__(S::WAVES * 64, 2) void int8_tiles_kernel(const TileParams a)
 {
     static_assert(S::WAVES == S2::WAVES, "one size of workgroup");
-    const uint32_t first = a.part[0].row_tiles * a.part[0].token_tiles;
-    if (blockIdx.x < first) tile<S, MATS, BACKWARD, ACT>(a, a.part[0], blockIdx.x);
-    else tile<S2, MATS, BACKWARD, ACT>(a, a.part[1], blockIdx.x - first);
+    const int first = (int)(a.part[0].row_tiles * a.part[0].token_tiles), block = tile_of_launch<S, MATS, BACKWARD>(a);
+    if (block < 0) return;
+    if (block < first) tile<S, MATS, BACKWARD, ACT>(a, a.part[0], (uint32_t)block);
+    else tile<S2, MATS, BACKWARD, ACT>(a, a.part[1], (uint32_t)(block - first));
 }
 
-hipError_t launch(void (*kernel)(const TileParams), int lds_bytes, int waves, const TileParams &p, hipStream_t stream)
+hipError_t launch(void (*kernel)(const TileParams), int lds_bytes, int waves, TileParams p, hipStream_t stream)
 {
     if (hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), lds_bytes)) return e;
     const uint32_t tiles = p.part[0].row_tiles * p.part[0].token_tiles + p.part[1].row_tiles * p.part[1].token_tiles;
-    hipLaunchKernelGGL(kernel, dim3(tiles), dim3(waves * 64), lds_bytes, stream, p);
+    p.sums_blocks = p.add_up ? (2 * p.m + waves * 64 - 1) / (waves * 64) : 0;
+    hipLaunchKernelGGL(kernel, dim3(p.sums_blocks + tiles), dim3(waves * 64), lds_bytes, stream, p);
     return hipGetLastError();
 }
 
@@ -504,7 +555,7 @@ TilePart part_of(uint32_t first_channel, uint32_t channels, uint32_t tokens)
 template <typename S, int MATS, bool BACKWARD, int ACT>
 hipError_t go(TileParams p, hipStream_t stream, int64_t &part_count)
 {
-    part_count = (p.tokens + S::FT * 32 - 1) / (S::FT * 32);
+    part_count = p.part_count = (p.tokens + S::FT * 32 - 1) / (S::FT * 32);
     p.part[0] = part_of<S, MATS>(0, p.m, p.tokens);
     return launch(int8_tile_kernel<S, MATS, BACKWARD, ACT>, TileLds<S, MATS, BACKWARD>::BYTES, S::WAVES, p, stream);
 }
@@ -514,7 +565,7 @@ template <typename S, typename S2, int MATS, bool BACKWARD, int ACT>
 hipError_t go_mixed(TileParams p, uint32_t first_row_tiles, hipStream_t stream, int64_t &part_count)
 {
     static_assert(S::FT == S2::FT, "partial sums over as many tokens");
-    part_count = (p.tokens + S::FT * 32 - 1) / (S::FT * 32);
+    part_count = p.part_count = (p.tokens + S::FT * 32 - 1) / (S::FT * 32);
     constexpr uint32_t CHANNELS = S::ROWS / MATS;
     constexpr int BYTES = TileLds<S, MATS, BACKWARD>::BYTES, BYTES2 = TileLds<S2, MATS, BACKWARD>::BYTES;
     p.part[0] = part_of<S, MATS>(0, first_row_tiles * CHANNELS, p.tokens);
@@ -624,14 +675,16 @@ hipError_t int8_tile_launch(const Int8Args &a, hipStream_t stream)
     return pick<false>(params(a), a.matrices, stream, part_count);
 }
 
-hipError_t int8_tile_backward_launch(const Int8Args &a, const Int8Workspace &ws, hipStream_t stream, int64_t &part_count)
+hipError_t int8_tile_backward_launch(const Int8Args &a, const Int8Workspace &ws, bool again, bool add_up, hipStream_t stream, int64_t &part_count)
 {
     TileParams p = params(a);
     unsigned char *base = static_cast<unsigned char *>(a.workspace);
     p.grad = reinterpret_cast<_Float16 *>(base + ws.grad);
-    p.norms = reinterpret_cast<const float *>(base + ws.norms);
-    p.scale_top = reinterpret_cast<const float *>(base + ws.scale_top);
-    p.typical = ws.typical;
+    p.powers = reinterpret_cast<const float *>(base + ws.powers);
+    p.fit = {reinterpret_cast<uint32_t *>(base + ws.some), reinterpret_cast<uint32_t *>(base + ws.other)};
+    p.again = again;
+    p.add_up = add_up;
+    for (int k = 0; k < 2; ++k) p.dscales[k] = a.dscales[k];
     p.parts = reinterpret_cast<float *>(base + ws.parts);
     p.grad_stride = (uint32_t)ws.grad_stride;
     p.m_padded = (uint32_t)(ws.grad_stride / a.matrices);

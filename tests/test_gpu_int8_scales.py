@@ -1,0 +1,198 @@
+"""Gradients of the 8-bit products where the scales, or what the codes make of them, lie far apart: against the definitions in 64 bits.
+
+The gradients of the projections, times their channels' scales, are held in binary16 between the two products of a backward pass: 11 bits, down to 2^-25
+of the token's largest (`gradients_error`).  The tolerances are made of the exact gradients alone.
+"""
+import pytest
+
+from tests.test_gpu_int8 import E32, act64, close, codes, generator, half_step, operands, sums64, sums_error, tiny
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def bcq():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    import paper_2510_10467_amd
+    return paper_2510_10467_amd
+
+
+def gradients_error(terms, matrices):
+    """What dx may be off by.  terms: (G, err) for each matrix, the exact gradients of its projections [tokens][m] times the channels' scales and their own
+    error in 32 bits.  Each is rounded to binary16: by half a step, 2^-11 of itself, or far below the token's largest by 2^-25 of that; then products with
+    codes, exact, and a chain of fp32 sums of 16 at a time, each off by 2^-24 of what it adds up, at most the sum of all magnitudes."""
+    largest = torch.stack([g.abs().amax(dim=1) for g, _ in terms]).amax(dim=0)[:, None]
+    k = sum(w.shape[0] for w in matrices)
+    return sum((err + (g.abs() + err) * (2.0 ** -11 + 8 * E32) + 2.0 ** -25 * largest) @ w.double().abs()
+               + (k / 16 + 40) * E32 * (g.abs() @ w.double().abs()) for (g, err), w in zip(terms, matrices))
+
+
+def gated64(dh, q, ts, wg, cg, wu, cu, activation):
+    """dx, the gradients of both sets of scales, and what each may be off by in 32 bits (dx: also by the rounding of the gradients)"""
+    d, cg, cu = dh.double(), cg.double(), cu.double()
+    pg, pu = (sums64(q, w) * ts.double()[:, None] for w in (wg, wu))
+    g, u = pg * cg, pu * cu
+    act, slope, sig, z, inner = act64(g, activation)
+    arg = 16 * z.abs() + 24                                     # roundings that an argument's error counts for
+    slope_err = E32 * (arg * (sig + g.abs() * sig * (1 - sig) * inner) + 6 * g.abs() * sig * inner)
+    dg, du = d * u * slope, d * act
+    dg_err, du_err = (d * u).abs() * slope_err + 8 * E32 * dg.abs(), du.abs() * arg * E32
+    dx = (dg * cg) @ wg.double() + (du * cu) @ wu.double()
+    dx_tol = gradients_error([(dg * cg, dg_err * cg.abs()), (du * cu, du_err * cu.abs())], [wg, wu])
+    dgate, dup = (dg * pg).sum(dim=0), (du * pu).sum(dim=0)
+    tokens = dh.shape[0]
+    return (dx, dgate, dup), (dx_tol, sums_error(dg * pg, (dg_err + 4 * E32 * dg.abs()) * pg.abs(), tokens) + 1e-40,
+                              sums_error(du * pu, (du_err + 4 * E32 * du.abs()) * pu.abs(), tokens) + 1e-40)
+
+
+def check_gated(bcq, dh, q, ts, wg, cg, wu, cu, activation, of_length=True):
+    """dh is first brought to where results are of the order of 2^8, by a power of two.  of_length: as a whole too a token's dx is off by no more than
+    independent roundings make, 2^-11 for the gradients of either matrix and half a step for the results: where rows of codes are no multiples of each other."""
+    dtype = dh.dtype
+    want, _ = gated64(dh, q, ts, wg, cg, wu, cu, activation)
+    size, most = float(want[0].abs().max()), float(dh.double().abs().max())
+    power = min(torch.tensor(256 / max(size, 1e-300)).log2().floor().item(), torch.tensor(2.0 ** 14 / most).log2().floor().item())
+    dh = (dh.double() * 2.0 ** power).to(dtype)
+    got = bcq.bcq_int8_gated_backward(dh, q, ts, wg, cg, wu, cu, activation)
+    want, tol = gated64(dh, q, ts, wg, cg, wu, cu, activation)
+    close(got[0], want[0], tol[0] + want[0].abs() * half_step(dtype) + tiny(dtype), "dx")
+    if of_length:
+        off = (got[0].double() - want[0]).norm(dim=1) - tiny(dtype) * want[0].shape[1] ** 0.5
+        assert bool((off <= want[0].norm(dim=1) * (2 * 2.0 ** -11 + half_step(dtype))).all()), float((off / want[0].norm(dim=1)).max())
+    close(got[1], want[1], tol[1], "dgate_scales")
+    close(got[2], want[2], tol[2], "dup_scales")
+    again = bcq.bcq_int8_gated_backward(dh, q, ts, wg, cg, wu, cu, activation)
+    assert all(torch.equal(a, b) for a, b in zip(again, got))
+
+
+DTYPES = [torch.float16, torch.bfloat16]
+SIZES = [(16, 1024, 1024), (3, 100, 48), (130, 300, 272), (600, 1100, 144)]
+
+
+@pytest.mark.parametrize("times", [2.0 ** 6, 2.0 ** 12, 2.0 ** 20, 2.0 ** 40])
+@pytest.mark.parametrize("matrix", ["gate", "up"])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tokens, m, n", SIZES)
+def test_a_row_of_zeros_with_a_large_scale(bcq, dtype, tokens, m, n, matrix, times):
+    """Quantisers give such a row whatever scale they like, 1.0 mostly.  It adds nothing to dx, but its gradient is there."""
+    gen = generator("zero row", tokens, m, n, matrix)
+    q, ts, [(wg, cg), (wu, cu)] = operands(tokens, m, n, gen, 2)
+    w, c = (wg, cg) if matrix == "gate" else (wu, cu)
+    w[m // 3], c[m // 3] = 0, times * float(c.max())
+    dh = torch.randn((tokens, m), device="cuda", generator=gen).to(dtype)
+    check_gated(bcq, dh, q, ts, wg, cg, wu, cu, "silu", times <= 2.0 ** 20)
+
+
+@pytest.mark.parametrize("times", [2.0 ** 6, 2.0 ** 12, 2.0 ** 20])
+@pytest.mark.parametrize("matrix", ["gate", "up"])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tokens, m, n", SIZES)
+def test_a_channel_with_a_large_scale(bcq, dtype, tokens, m, n, matrix, times):
+    """... whose gradient counts, and for every second token none of its own (dh = 0 there): the other channels' then are all there is."""
+    gen = generator("large scale", tokens, m, n, matrix)
+    q, ts, [(wg, cg), (wu, cu)] = operands(tokens, m, n, gen, 2)
+    c = cg if matrix == "gate" else cu
+    c[m // 2] *= times
+    dh = torch.randn((tokens, m), device="cuda", generator=gen).to(dtype)
+    dh[::2, m // 2] = 0
+    check_gated(bcq, dh, q, ts, wg, cg, wu, cu, "gelu")
+
+
+@pytest.mark.parametrize("times", [2.0 ** -10, 2.0 ** -20, 2.0 ** -40])
+@pytest.mark.parametrize("matrix", ["gate", "up"])
+@pytest.mark.parametrize("activation", ["silu", "gelu"])
+@pytest.mark.parametrize("tokens, m, n", SIZES)
+def test_scales_of_gate_and_up_far_apart(bcq, activation, tokens, m, n, matrix, times):
+    gen = generator("apart", tokens, m, n, matrix)
+    q, ts, [(wg, cg), (wu, cu)] = operands(tokens, m, n, gen, 2)
+    (cg if matrix == "gate" else cu).mul_(times)
+    dh = torch.randn((tokens, m), device="cuda", generator=gen).bfloat16()
+    check_gated(bcq, dh, q, ts, wg, cg, wu, cu, activation)
+
+
+@pytest.mark.parametrize("largest", [1, 6, 127])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tokens, m, n", SIZES)
+def test_codes_of_any_size(bcq, dtype, tokens, m, n, largest):
+    """Any codes are legal, those of -1 to 1 with scales as much larger too."""
+    gen = generator("codes", tokens, m, n, largest)
+    q, ts, _ = operands(tokens, m, n, gen)
+    size = 2.0 / (0.01 * 73 * 73 * n ** 0.5) * (127 / largest)
+    q = (q.float() * (largest / 127)).round().to(torch.int8)
+    ts = ts * (127 / largest)
+    wg, wu = (torch.randint(-largest, largest + 1, (m, n), dtype=torch.int8, device="cuda", generator=gen) for _ in range(2))
+    cg, cu = ((0.5 + torch.rand(m, device="cuda", generator=gen)) * size for _ in range(2))
+    dh = torch.randn((tokens, m), device="cuda", generator=gen).to(dtype)
+    check_gated(bcq, dh, q, ts, wg, cg, wu, cu, "silu")
+
+
+@pytest.mark.parametrize("activation, lowest", [("silu", -24.0), ("silu", -60.0), ("gelu", -5.0)])
+@pytest.mark.parametrize("tokens, m, n", SIZES)
+def test_gates_that_are_shut(bcq, activation, lowest, tokens, m, n):
+    """Every second token's gates are all far below zero: its gradients are tiny, and as exact as any."""
+    gen = generator("shut", tokens, m, n, activation, lowest)
+    q, ts, [(wg, cg), (wu, cu)] = operands(tokens, m, n, gen, 2)
+    q[::2] = q[::2].abs().clamp_min(40)
+    wg = -wg.abs().clamp_min(40)
+    g = sums64(q, wg) * ts.double()[:, None]
+    cg = (cg.double() * lowest / (g * cg.double())[::2].min()).float()
+    dh = torch.randn((tokens, m), device="cuda", generator=gen).bfloat16()
+    check_gated(bcq, dh, q, ts, wg, cg, wu, cu, activation)
+
+
+@pytest.mark.parametrize("tokens, m, n", SIZES)
+def test_sums_beyond_the_typical(bcq, tokens, m, n):
+    """All codes of one sign and size: the largest gradients for their scales, and among them channels without any (their codes cancel)."""
+    gen = generator("beyond", tokens, m, n)
+    q, ts, [(wg, cg), (wu, cu)] = operands(tokens, m, n, gen, 2)
+    q.fill_(-128)
+    q[1::2] = 1
+    wg[: m // 2], wu[: m // 2] = -128, -128
+    wg[m // 2:, ::2], wg[m // 2:, 1::2] = 100, -100
+    cg, cu = cg * 73 / 128 / n ** 0.5, cu * 73 / 128 / n ** 0.5
+    dh = torch.randn((tokens, m), device="cuda", generator=gen).half()
+    check_gated(bcq, dh, q, ts, wg, cg, wu, cu, "silu", False)
+
+
+def test_a_token_of_any_other(bcq):
+    """What a token's gradients are held at is its own: tokens of very different kinds beside each other, and each alone, give the same bits."""
+    gen = generator("kinds")
+    tokens, m, n = 70, 300, 272
+    q, ts, [(wg, cg), (wu, cu)] = operands(tokens, m, n, gen, 2)
+    wg[7], cg[7] = 0, 2.0 ** 30
+    ts = ts * torch.exp2(torch.randint(-30, 3, (tokens,), device="cuda", generator=gen).float())
+    dh = torch.randn((tokens, m), device="cuda", generator=gen)
+    dh = (dh * torch.exp2(torch.randint(-20, 20, (tokens, 1), device="cuda", generator=gen).float())).bfloat16()
+    dh[::3, 7] = 0
+    dh[5], ts[6] = 0, 0
+    want, tol = gated64(dh, q, ts, wg, cg, wu, cu, "silu")
+    got = bcq.bcq_int8_gated_backward(dh, q, ts, wg, cg, wu, cu)[0]
+    close(got, want[0], tol[0] + want[0].abs() * half_step(torch.bfloat16) + tiny(torch.bfloat16), "dx")
+    dh[8, 3], ts[9], q[9] = float("nan"), float("nan"), 0
+    other = bcq.bcq_int8_gated_backward(dh, q, ts, wg, cg, wu, cu)[0]
+    keep = [t for t in range(tokens) if t not in (8, 9)]
+    assert torch.equal(other[keep], got[keep]) and bool(other[[8, 9]].isnan().all())
+
+
+@pytest.mark.parametrize("times", [2.0 ** 12, 2.0 ** 24, 2.0 ** 40])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tokens, m, n", SIZES)
+def test_gemm_with_a_large_scale(bcq, dtype, tokens, m, n, times):
+    """One matrix: every second token has no gradient at the channel with the large scale, the others' other channels do not count beside it."""
+    gen = generator("gemm scale", tokens, m, n)
+    q, ts, [(w, cs)] = operands(tokens, m, n, gen)
+    cs[m // 2] *= times
+    dy = torch.randn((tokens, m), device="cuda", generator=gen).to(dtype)
+    dy[:, m // 2] = (dy[:, m // 2].float() / min(times, 2.0 ** 14)).to(dtype)
+    dy[::2, m // 2] = 0
+    dx, dc = bcq.bcq_int8_gemm_backward(dy, q, ts, w, cs)
+    d, c, w64 = dy.double(), cs.double(), w.double()
+    ref = (d * c) @ w64
+    assert float(ref[::2].abs().max()) < 2.0 ** 15
+    fits = ref.abs() < 2.0 ** 15 if dtype == torch.float16 else torch.ones_like(ref, dtype=torch.bool)
+    tol = gradients_error([(d * c, 2 * E32 * (d * c).abs())], [w]) + ref.abs() * half_step(dtype) + tiny(dtype)
+    close(torch.where(fits, dx.double(), 0.0), torch.where(fits, ref, 0.0), tol, "dx")
+    terms = d * sums64(q, w) * ts.double()[:, None]
+    close(dc, terms.sum(dim=0), sums_error(terms, 4 * E32 * terms.abs(), tokens) + 1e-40, "dchannel_scales")
