@@ -46,6 +46,8 @@ def _load_host(functions, int8_functions):
         from . import _bcq_host as host
         if host.torch_version != torch.__version__:
             raise ImportError(f"built for torch {host.torch_version}, this is {torch.__version__}")
+        if not hasattr(host, "bind_int8"):
+            raise ImportError("built before the 8-bit operators")
     except ImportError as e:
         warnings.warn(f"_bcq_host does not load ({e}); calls from Python take about 5 us longer until the package is built again "
                       "(`python paper_2510_10467_amd/build.py`)", RuntimeWarning, stacklevel=3)
