@@ -80,6 +80,18 @@ int bcq_mixed_shape_for(int precisions, int64_t m, int64_t n, int batch, int gro
  */
 int bcq_level_layout(int p, int row_blocks, int64_t n, int group, int with_offsets, int *layout);
 
+/*
+ * What the 8-bit products of these sizes run on (matrices: 1, or 2 for the gated block; backward: 0 or 1; tensors aligned to 128 bytes):
+ *   layout[0]   0: rows of weights streamed by each wave, 1: tiles, 2: full rounds of tiles and then tiles of half the tokens in one launch
+ *   layout[1]   rows of weights of a workgroup (of all matrices), [2] its tokens, [3] columns of a step, [4] teams of waves that share out the steps (streamed
+ *               rows: waves), [5] steps that a team's buffers hold, [6] steps that the first team takes, [7] bytes of LDS
+ *   backward, the product with the weights' rows, zeros otherwise:
+ *   layout[8]   columns of a workgroup, [9] its tokens, [10] teams, [11] steps that a team's buffers hold, [12] steps that the first team takes, [13] runs that the
+ *               channels are taken in, [14] bytes of LDS
+ * Needs no GPU.  Returns 0, -1 NULL, or -3 for sizes that the calls refuse, and for no tokens.
+ */
+int bcq_int8_layout(int matrices, int backward, int64_t m, int64_t n, int64_t tokens, int *layout);
+
 /* Name of the variant the calling thread's most recent successful launch used ("" before any): "sign_select",
  * "lut", "plane_mfma" ("plane_mfma_rows" where that family ran in its row-streaming form: tall matrices with two to eight
  * requests, or with one request at one or two planes), "dequant_mfma", "plane_f16", "quantize"; of the 8-bit operators "int8_quantize", "int8_rows"

@@ -79,6 +79,8 @@ def lib() -> ctypes.CDLL:
         L.bcq_mixed_shape_for.restype = i32
         L.bcq_level_layout.argtypes = [i32, i32, i64, i32, i32, vp]
         L.bcq_level_layout.restype = i32
+        L.bcq_int8_layout.argtypes = [i32, i32, i64, i64, i64, vp]
+        L.bcq_int8_layout.restype = i32
         L.bcq_pack.argtypes = [vp, vp, i32, i64, i64, vp]
         L.bcq_unpack.argtypes = [vp, vp, i32, i64, i64, vp]
         L.bcq_gemv.argtypes = [vp, vp, i32, vp, vp, i64, i64, i32, i32, vp]
@@ -168,6 +170,17 @@ def level_layout(p: int, row_blocks: int, n: int, group: int = 128, with_offsets
     got = (ctypes.c_int * 4)()
     _check(lib().bcq_level_layout(p, row_blocks, n, group, int(with_offsets), got), "bcq_level_layout")
     return dict(zip(("lds_bytes", "window_columns", "window_loads", "word_columns"), got))
+
+
+def int8_layout(m: int, n: int, tokens: int, matrices: int = 1, backward: bool = False) -> dict:
+    """Benchmarks and tests: what the 8-bit products of these sizes run on; ``kernel`` is "rows", "tiles" or "mixed" (tiles of two shapes)."""
+    got = (ctypes.c_int * 15)()
+    _check(lib().bcq_int8_layout(matrices, int(backward), m, n, tokens, got), "bcq_int8_layout")
+    names = ("rows", "tokens", "step", "teams", "ring", "rounds", "lds_bytes")
+    layout = dict(zip(names, got[1:8]), kernel=("rows", "tiles", "mixed")[got[0]])
+    if backward:
+        layout["second"] = dict(zip(("columns", "tokens", "teams", "ring", "rounds", "runs", "lds_bytes"), got[8:]))
+    return layout
 
 
 def last_kernel() -> str:

@@ -510,6 +510,23 @@ int bcq_int8_gated(const int8_t *q, const float *token_scales, const int8_t *w_g
     return run_int8(int8_args(q, token_scales, w_gate, gate_scales, w_up, up_scales, 2, activation, h, type, m, n, tokens), stream);
 }
 
+int bcq_int8_layout(int matrices, int backward, int64_t m, int64_t n, int64_t tokens, int *layout)
+{
+    if (!layout) return BCQ_ERR_NULL;
+    if (matrices < 1 || matrices > 2 || tokens < 1) return BCQ_ERR_BAD_SHAPE;
+    if (int rc = check_int8(BCQ_FLOAT16, BCQ_ACT_SILU, m, n, tokens, backward ? kInt8MaxBackwardRows : kInt8MaxRows)) return rc;
+    const bcq::Int8Args a = int8_args(nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, matrices, BCQ_ACT_SILU, nullptr, BCQ_FLOAT16, m, n, tokens);
+    const bool rows = !backward && bcq::int8_rows_supports(a);
+    bool mixed = false;
+    int runs = 0;
+    const bcq::Int8Layout first = rows ? bcq::int8_rows_layout(a) : bcq::int8_tile_layout(a, backward != 0, mixed);
+    const bcq::Int8Layout second = backward ? bcq::int8_second_layout(a, runs) : bcq::Int8Layout{};
+    const int all[15] = {rows ? 0 : mixed ? 2 : 1, first.rows, first.tokens, first.step, first.teams, first.ring, first.rounds, first.lds_bytes,
+                         second.rows, second.tokens, second.teams, second.ring, second.rounds, runs, second.lds_bytes};
+    for (int i = 0; i < 15; ++i) layout[i] = all[i];
+    return BCQ_OK;
+}
+
 int64_t bcq_int8_backward_workspace(int matrices, int64_t m, int64_t n, int64_t tokens)
 {
     if (matrices < 1 || matrices > 2) return BCQ_ERR_BAD_SHAPE;

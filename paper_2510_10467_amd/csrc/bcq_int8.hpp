@@ -113,12 +113,19 @@ __device__ __forceinline__ float sum_of_parts(const float *parts, int64_t count,
 
 hipError_t int8_quantize_launch(const uint16_t *x, bool bf16, int8_t *q, float *scales, int64_t rows, int64_t n, hipStream_t stream);
 
+// What a workgroup of the products takes and keeps, as bcq_int8_layout has it
+struct Int8Layout {
+    int rows, tokens, step, teams, ring, rounds, lds_bytes;
+};
+
 // Few tokens: every wave streams rows of weights through LDS of its own.
 bool int8_rows_supports(const Int8Args &a);
 hipError_t int8_rows_launch(const Int8Args &a, hipStream_t stream);
+Int8Layout int8_rows_layout(const Int8Args &a);
 
 // Any number of tokens: tiles of both operands in LDS.
 hipError_t int8_tile_launch(const Int8Args &a, hipStream_t stream);
+Int8Layout int8_tile_layout(const Int8Args &a, bool backward, bool &mixed);
 
 // The backward passes' workspace, in this order.
 struct Int8Workspace {
@@ -133,5 +140,7 @@ Int8Workspace int8_workspace(int matrices, int64_t m, int64_t n, int64_t tokens)
 // fit, and with add_up the partial sums' sums.
 hipError_t int8_tile_backward_launch(const Int8Args &a, const Int8Workspace &ws, bool again, bool add_up, hipStream_t stream, int64_t &part_count);
 hipError_t int8_backward_launch(const Int8Args &a, hipStream_t stream);
+// of the second product (rows: columns)
+Int8Layout int8_second_layout(const Int8Args &a, int &runs);
 
 }  // namespace bcq

@@ -528,6 +528,21 @@ Int8Workspace int8_workspace(int matrices, int64_t m, int64_t n, int64_t tokens)
     return ws;
 }
 
+Int8Layout int8_second_layout(const Int8Args &a, int &runs)
+{
+    const SecondPlan plan = second_plan(a.matrices, a.m, a.n, a.tokens);
+    runs = plan.splits;
+    Int8Layout layout{};
+    int index = 0;
+    for_shapes([&](auto shape, float, float) {
+        using S = decltype(shape);
+        if (index++ != plan.shape) return;
+        const int64_t steps = a.matrices * ((a.m + 63) / 64), run = (steps + runs - 1) / runs;
+        layout = {S::COLS, S::TOKS, S::STEP, S::TEAMS, S::RING, (int)((run + S::TEAMS - 1) / S::TEAMS), S::BYTES};
+    });
+    return layout;
+}
+
 hipError_t int8_backward_launch(const Int8Args &a, hipStream_t stream)
 {
     const Int8Workspace ws = int8_workspace(a.matrices, a.m, a.n, a.tokens);

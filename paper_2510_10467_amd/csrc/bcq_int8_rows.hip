@@ -181,15 +181,14 @@ __global__ __launch_bounds__(S::WAVES * 64) void int8_rows_kernel(const RowsPara
     }
 }
 
-template <int TT, int MATS, int BLOCKS, int WAVES, int RING>
+template <typename S>
 hipError_t go(const RowsParams &p, hipStream_t stream)
 {
-    using S = RowsShape<TT, MATS, BLOCKS, WAVES, RING>;
     static_assert(S::BYTES <= 160 * 1024, "LDS of a CU");
-    const int64_t blocks = (p.m + 16 * BLOCKS - 1) / (16 * BLOCKS);
+    const int64_t blocks = (p.m + 16 * S::BLOCKS - 1) / (16 * S::BLOCKS);
     const auto kernel = int8_rows_kernel<S>;
     if (hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), S::BYTES)) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks, (unsigned)((p.tokens + S::TT * 16 - 1) / (S::TT * 16))), dim3(WAVES * 64), S::BYTES, stream, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks, (unsigned)((p.tokens + S::TT * 16 - 1) / (S::TT * 16))), dim3(S::WAVES * 64), S::BYTES, stream, p);
     return hipGetLastError();
 }
 
@@ -208,25 +207,25 @@ int tokens_of(int64_t m, int64_t tokens, int matrices)
     return tokens <= 32 && matrices == 1 && m <= 16384 ? 32 : 0;
 }
 
-template <int MATS>
-hipError_t pick(const RowsParams &p, hipStream_t stream)
+template <int MATS, typename F>
+auto with_shape(int64_t m, int64_t tokens, F f)
 {
     // More tokens' codes are worth two blocks of rows, where those still give every CU a workgroup: 14336 x 4096 with 32 tokens 13.6 -> 11.0 us
     // (4096 x 14336 the other way, 11.0 against 15.7); 35840 x 5120 with 16 tokens 41.4 -> 36.5 (with 8 tokens 34.0 both, gated
     // 17920 x 5120 with 16 tokens the other way, 37.2 against 41.5).
-    const int some = tokens_of(p.m, p.tokens, MATS);
-    if (p.tokens <= 8) return go<0, MATS, 1, 4, 3>(p, stream);
+    const int some = tokens_of(m, tokens, MATS);
+    if (tokens <= 8) return f(RowsShape<0, MATS, 1, 4, 3>{});
     if (some == 16) {
         if constexpr (MATS == 1)
-            if (p.m >= 16384) return go<1, 1, 2, 4, 3>(p, stream);
-        return go<1, MATS, 1, 4, 3>(p, stream);
+            if (m >= 16384) return f(RowsShape<1, 1, 2, 4, 3>{});
+        return f(RowsShape<1, MATS, 1, 4, 3>{});
     }
     if (some == 32) {
         if constexpr (MATS == 1)
-            if (p.m >= 8192) return go<2, 1, 2, 4, 2>(p, stream);
-        return go<2, MATS, 1, 4, 3>(p, stream);
+            if (m >= 8192) return f(RowsShape<2, 1, 2, 4, 2>{});
+        return f(RowsShape<2, MATS, 1, 4, 3>{});
     }
-    return go<4, MATS, 1, 4, 3>(p, stream);
+    return f(RowsShape<4, MATS, 1, 4, 3>{});
 }
 
 }  // namespace
@@ -237,7 +236,18 @@ hipError_t int8_rows_launch(const Int8Args &a, hipStream_t stream)
 {
     const RowsParams p{a.q, {a.w[0], a.w[1]}, a.token_scales, {a.channel_scales[0], a.channel_scales[1]}, a.y, a.m, (int)a.n, (int)a.tokens,
                        a.activation, a.bf16};
-    return a.matrices == 2 ? pick<2>(p, stream) : pick<1>(p, stream);
+    auto run = [&](auto shape) { return go<decltype(shape)>(p, stream); };
+    return a.matrices == 2 ? with_shape<2>(a.m, a.tokens, run) : with_shape<1>(a.m, a.tokens, run);
+}
+
+Int8Layout int8_rows_layout(const Int8Args &a)
+{
+    auto layout = [&](auto shape) {
+        using S = decltype(shape);
+        const int steps = (int)((a.n + kStep - 1) / kStep);
+        return Int8Layout{16 * S::WF, S::Q_LOADS == 1 ? 8 : 16 * S::TT, kStep, S::WAVES, S::RING, (steps + S::WAVES - 1) / S::WAVES, S::BYTES};
+    };
+    return a.matrices == 2 ? with_shape<2>(a.m, a.tokens, layout) : with_shape<1>(a.m, a.tokens, layout);
 }
 
 }  // namespace bcq

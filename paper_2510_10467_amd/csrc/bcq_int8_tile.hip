@@ -603,16 +603,21 @@ void for_shapes(F f)
     f(TileShape<1, 1, 2, 1, 3, 4>{}, 0.20f, 0.20f);         // 64 x 32, four teams
 }
 
-template <int MATS, bool BACKWARD, int ACT>
-hipError_t pick(const TileParams &p, hipStream_t stream, int64_t &part_count)
+// The shape, by its place among for_shapes, or the largest tiles in so many tiles of rows and Large behind them.
+struct TileChoice {
+    int shape;
+    uint32_t first_row_tiles;
+};
+template <int MATS>
+TileChoice choose(uint32_t m, uint32_t n, uint32_t tokens, bool aligned)
 {
-    const bool lines = p.n % 128 == 0 && ((reinterpret_cast<uintptr_t>(p.w[0]) | reinterpret_cast<uintptr_t>(p.w[MATS - 1])) & 127) == 0;
+    const bool lines = n % 128 == 0 && aligned;
     float best = 0.f;
     int index = 0, chosen = -1;
     for_shapes([&](auto shape, float alone, float in_turn) {
         using S = decltype(shape);
         if (S::STEP < 128 && !lines) alone = in_turn = 1e9f;
-        const int64_t tiles = (int64_t)((p.m * MATS + S::ROWS - 1) / S::ROWS) * ((p.tokens + S::TOKS - 1) / S::TOKS);
+        const int64_t tiles = (int64_t)((m * MATS + S::ROWS - 1) / S::ROWS) * ((tokens + S::TOKS - 1) / S::TOKS);
         const int64_t each = (tiles + 255) / 256;                   // tiles of the busiest CU
         const float us = each == 1 ? alone : (float)each * in_turn;
         if (chosen < 0 || us < best) {
@@ -623,18 +628,26 @@ hipError_t pick(const TileParams &p, hipStream_t stream, int64_t &part_count)
     });
     // The largest tiles as far as they fill rounds, and where one round of those of half the tokens takes what is left, that (2048 tokens, 4096
     // columns, gated, 14336 rows, 3.5 rounds: 247 -> 231 us; 12288 rows, three rounds: 189).
-    const TilePart all = part_of<Largest, MATS>(0, p.m, p.tokens);
+    const TilePart all = part_of<Largest, MATS>(0, m, tokens);
     const int64_t rounds = (int64_t)all.row_tiles * all.token_tiles / 256;
     const uint32_t first = (uint32_t)(rounds * 256 / all.token_tiles);
     if (rounds > 0 && first < all.row_tiles) {
-        const TilePart left = part_of<Large, MATS>(0, (all.row_tiles - first) * (Largest::ROWS / MATS), p.tokens);
-        if ((int64_t)left.row_tiles * left.token_tiles <= 256 && (float)rounds * kLargestUs + kLargeUs < best)
-            return go_mixed<Largest, Large, MATS, BACKWARD, ACT>(p, first, stream, part_count);
+        const TilePart left = part_of<Large, MATS>(0, (all.row_tiles - first) * (Largest::ROWS / MATS), tokens);
+        if ((int64_t)left.row_tiles * left.token_tiles <= 256 && (float)rounds * kLargestUs + kLargeUs < best) return {0, first};
     }
+    return {chosen, 0};
+}
+
+template <int MATS, bool BACKWARD, int ACT>
+hipError_t pick(const TileParams &p, hipStream_t stream, int64_t &part_count)
+{
+    const bool aligned = ((reinterpret_cast<uintptr_t>(p.w[0]) | reinterpret_cast<uintptr_t>(p.w[MATS - 1])) & 127) == 0;
+    const TileChoice choice = choose<MATS>(p.m, p.n, p.tokens, aligned);
+    if (choice.first_row_tiles) return go_mixed<Largest, Large, MATS, BACKWARD, ACT>(p, choice.first_row_tiles, stream, part_count);
     hipError_t result = hipErrorInvalidValue;
-    index = 0;
+    int index = 0;
     for_shapes([&](auto shape, float, float) {
-        if (index++ == chosen) result = go<decltype(shape), MATS, BACKWARD, ACT>(p, stream, part_count);
+        if (index++ == choice.shape) result = go<decltype(shape), MATS, BACKWARD, ACT>(p, stream, part_count);
     });
     return result;
 }
@@ -644,6 +657,20 @@ hipError_t pick(const TileParams &p, int matrices, hipStream_t stream, int64_t &
 {
     if (matrices == 1) return pick<1, BACKWARD, BCQ_ACT_SILU>(p, stream, part_count);
     return p.activation == BCQ_ACT_GELU ? pick<2, BACKWARD, BCQ_ACT_GELU>(p, stream, part_count) : pick<2, BACKWARD, BCQ_ACT_SILU>(p, stream, part_count);
+}
+
+template <int MATS, bool BACKWARD>
+Int8Layout layout_of(const TileChoice &choice, uint32_t n)
+{
+    Int8Layout layout{};
+    int index = 0;
+    for_shapes([&](auto shape, float, float) {
+        using S = decltype(shape);
+        if (index++ != choice.shape) return;
+        const int steps = (int)((n + S::STEP - 1) / S::STEP);
+        layout = {S::ROWS, S::TOKS, S::STEP, S::TEAMS, S::RING, (steps + S::TEAMS - 1) / S::TEAMS, TileLds<S, MATS, BACKWARD>::BYTES};
+    });
+    return layout;
 }
 
 TileParams params(const Int8Args &a)
@@ -673,6 +700,15 @@ hipError_t int8_tile_launch(const Int8Args &a, hipStream_t stream)
 {
     int64_t part_count;
     return pick<false>(params(a), a.matrices, stream, part_count);
+}
+
+Int8Layout int8_tile_layout(const Int8Args &a, bool backward, bool &mixed)
+{
+    const uint32_t m = (uint32_t)a.m, n = (uint32_t)a.n, tokens = (uint32_t)a.tokens;
+    const TileChoice choice = a.matrices == 2 ? choose<2>(m, n, tokens, true) : choose<1>(m, n, tokens, true);
+    mixed = choice.first_row_tiles > 0;
+    if (a.matrices == 2) return backward ? layout_of<2, true>(choice, n) : layout_of<2, false>(choice, n);
+    return backward ? layout_of<1, true>(choice, n) : layout_of<1, false>(choice, n);
 }
 
 hipError_t int8_tile_backward_launch(const Int8Args &a, const Int8Workspace &ws, bool again, bool add_up, hipStream_t stream, int64_t &part_count)

@@ -169,9 +169,8 @@ def test_quantize_zero_and_unfit_rows(bcq, dtype, rows):
 # few tokens and tiles of 64, ends of every kind: rows, tokens, columns (16, 32, 48, 64, .. over a step of 128), one to many steps
 SIZES = [(1, 1, 16), (1, 16, 32), (2, 40, 48), (5, 17, 64), (16, 100, 112), (15, 1000, 4096), (1, 129, 1040), (3, 33, 14336),
          (17, 1, 16), (17, 40, 48), (33, 64, 128), (64, 65, 144), (77, 101, 1040), (130, 129, 80), (300, 200, 2064), (65, 1000, 272)]
-# tall and short matrices with few tokens, and each tile shape of many rows and tokens: 256 x 128, 256 x 256, 128 x 128, 128 x 64 (rows of
-# whole 128 bytes and others), 256 x 64, 192 x 64, 192 x 128, and 256 x 256 with 256 x 128 behind them, 64 x 64, 64 x 32; short
-# matrices with 16, 32 and 64 tokens in a workgroup
+# tall and short matrices with few to many tokens.  (Which kernels these run on is up to the prices; tests/test_gpu_int8_shapes.py has sizes that are held to
+# reach every one.)
 LARGE_SIZES = [(12, 16400, 144), (20, 8200, 272), (40, 9000, 144), (200, 16400, 144), (129, 20000, 272), (300, 33001, 208), (257, 33024, 1040),
                (500, 28600, 80), (100, 20010, 144), (100, 10001, 272), (40, 33000, 400), (64, 36001, 1040),
                (300, 48100, 80), (500, 47000, 272), (100, 20010, 256), (100, 10001, 1152),
