@@ -1,4 +1,4 @@
-"""What the 8-bit products run on: host code, no GPU needed."""
+"""What the 8-bit products run on: host code and the built kernels' resources, no GPU needed."""
 import itertools
 
 import pytest
@@ -6,6 +6,7 @@ import pytest
 import paper_2510_10467_amd as bcq
 from paper_2510_10467_amd import build as hip_build
 from tests import test_gpu_int8_shapes as gpu
+from tests.test_kernel_resources import kernels      # noqa: F401  (a fixture)
 
 # rows x tokens, columns of a step, teams, steps that a ring holds
 TILES = {(256, 256, 128, 1, 2), (256, 128, 128, 1, 3), (128, 128, 128, 1, 4), (256, 64, 128, 1, 4), (192, 128, 128, 1, 4), (192, 64, 128, 1, 5),
@@ -86,3 +87,26 @@ def test_layout_refuses_what_the_calls_refuse():
             bcq.int8_layout(m, 64, 4, matrices, backward)
         assert error.value.status == -3
     assert bcq.lib().bcq_int8_layout(1, 0, 8, 64, 4, None) == -1
+
+
+def test_no_kernel_spills(kernels):                  # noqa: F811
+    eight_bit = {name: use for name, use in kernels.items() if "int8_" in name}
+    # per number of matrices (with two, per activation) and direction ten shapes of tiles and the mixed launch; streamed rows; the second product
+    assert len([name for name in eight_bit if "int8_tile" in name]) == 11 * 3 * 2
+    assert len([name for name in eight_bit if "int8_rows" in name]) == 10
+    assert len([name for name in eight_bit if "int8_second" in name]) == 4
+    for name, (registers, scratch) in eight_bit.items():
+        assert scratch == 0, f"{name}: {scratch} bytes of scratch"
+
+
+def test_two_workgroups_of_the_second_product_share_a_cu(kernels):      # noqa: F811
+    """Its prices for 128 columns x 128 tokens and 128 x 64 count on two per CU: 160 KiB of LDS and, four and eight waves a workgroup, 256 and 128
+    vector registers a lane."""
+    for waves, (m, n, tokens), shape in ((4, (403, 9136, 76), (128, 128, 1, 3)), (8, (752, 8800, 401), (128, 64, 2, 2))):
+        layout = bcq.int8_layout(m, n, tokens, 1, True)
+        assert second(layout)[0] == shape
+        assert 2 * layout["second"]["lds_bytes"] <= 160 * 1024
+        teams, ring = shape[2], shape[3]
+        mangled = f"int8_second_kernelINS0_11SecondShapeILi4ELi1ELi1ELi{shape[1] // 32}ELi{ring}ELi{teams}E"
+        found = [use for name, use in kernels.items() if mangled in name]
+        assert len(found) == 1 and found[0][0] <= 512 // (2 * waves // 4)
