@@ -196,3 +196,25 @@ def test_gemm_with_a_large_scale(bcq, dtype, tokens, m, n, times):
     close(torch.where(fits, dx.double(), 0.0), torch.where(fits, ref, 0.0), tol, "dx")
     terms = d * sums64(q, w) * ts.double()[:, None]
     close(dc, terms.sum(dim=0), sums_error(terms, 4 * E32 * terms.abs(), tokens) + 1e-40, "dchannel_scales")
+
+
+@pytest.mark.parametrize("dtype, exponents", [(torch.float16, (-10, -6, 6, 12)), (torch.bfloat16, (-120, -60, 60, 110))])
+def test_gradients_near_either_end_of_the_type(bcq, dtype, exponents):
+    """A power of two on dy changes nothing but the results' exponents, where these have room for it."""
+    gen = generator("ends")
+    tokens, m, n = 6, 24, 64
+    q, ts, [(wg, cg), (wu, cu)] = operands(tokens, m, n, gen, 2)
+    size = torch.randint(8, 16, (tokens, m), device="cuda", generator=gen) / 8.0 * torch.exp2(torch.randint(-3, 2, (tokens, m), device="cuda", generator=gen).float())
+    base = torch.where(torch.rand((tokens, m), device="cuda", generator=gen) < 0.5, -size, size).to(dtype)
+    for call in (lambda d: bcq.bcq_int8_gated_backward(d, q, ts, wg, cg, wu, cu), lambda d: bcq.bcq_int8_gemm_backward(d, q, ts, wg, cg)):
+        want = call(base)
+        for e in exponents:
+            dy = (base.double() * 2.0 ** e).to(dtype)
+            assert torch.equal(dy.double() * 2.0 ** -e, base.double())           # (four bits, all in the normal range)
+            got = call(dy)
+            ref = want[0].double() * 2.0 ** e
+            assert float(ref.abs().max()) < torch.finfo(dtype).max
+            # (both are roundings of the same sums, but where those leave fp32's or the type's normal range)
+            close(got[0], ref, 2 * half_step(dtype) * ref.abs() + 2 * tiny(dtype), f"dx, 2^{e}")
+            for a, b in zip(got[1:], want[1:]):
+                close(a, b.double() * 2.0 ** e, 2 * E32 * (b.double() * 2.0 ** e).abs() + 1e-40, f"scales, 2^{e}")
