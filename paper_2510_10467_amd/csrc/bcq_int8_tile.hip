@@ -597,7 +597,8 @@ void for_shapes(F f)
     f(TileShape<3, 2, 2, 1, 5>{}, 0.62f, 0.66f);
     f(TileShape<2, 1, 2, 2, 6, 2, 64>{}, 0.34f, 0.50f);     // 128 x 64, two teams
     // ... where rows are no whole lines: a piece of 64 bytes is then a line's half with one round and the other with the next (25065 x 6800 with 34
-    // tokens 50.7 -> 42.7 us, 8448 x 11680 gated with 17 65 -> 57; on whole lines 4096 x 14336 with 512 the other way, 41.7 against 47.7)
+    // tokens 50.7 -> 42.7 us, 8448 x 11680 gated with 17 65 -> 57).  On whole lines it depends on where the weights are: 4096 x 14336 with 512 tokens 42
+    // against 47 us where they are in the last cache, 57 against 51 where they come from memory.
     f(TileShape<2, 1, 2, 2, 3, 2>{}, 0.34f, 0.50f);
     f(TileShape<1, 2, 2, 1, 4, 2>{}, 0.28f, 0.30f);         // 64 x 64, two teams
     f(TileShape<1, 1, 2, 1, 3, 4>{}, 0.20f, 0.20f);         // 64 x 32, four teams
@@ -617,6 +618,9 @@ TileChoice choose(uint32_t m, uint32_t n, uint32_t tokens, bool aligned)
     for_shapes([&](auto shape, float alone, float in_turn) {
         using S = decltype(shape);
         if (S::STEP < 128 && !lines) alone = in_turn = 1e9f;
+        // Two matrices with rows 8 KiB apart: 192 x 64 are behind 256 x 64 (24576 rows of each with 64 tokens 78 against 70 us; 8064 columns 71 against
+        // 85, 8320 columns 72 against 86, one matrix of 49152 rows 72 against 73).
+        if (MATS == 2 && S::ROWS == 192 && S::TOKS == 64 && n == 8192) alone = 0.70f;
         const int64_t tiles = (int64_t)((m * MATS + S::ROWS - 1) / S::ROWS) * ((tokens + S::TOKS - 1) / S::TOKS);
         const int64_t each = (tiles + 255) / 256;                   // tiles of the busiest CU
         const float us = each == 1 ? alone : (float)each * in_turn;

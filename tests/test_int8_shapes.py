@@ -110,3 +110,13 @@ def test_two_workgroups_of_the_second_product_share_a_cu(kernels):      # noqa: 
         mangled = f"int8_second_kernelINS0_11SecondShapeILi4ELi1ELi1ELi{shape[1] // 32}ELi{ring}ELi{teams}E"
         found = [use for name, use in kernels.items() if mangled in name]
         assert len(found) == 1 and found[0][0] <= 512 // (2 * waves // 4)
+
+
+# (matrices, m, n, tokens): microseconds on one MI355X of the tiles of 192 x 64 and of 256 x 64
+@pytest.mark.parametrize("call, of_192, of_256", [((2, 17920, 5120, 48), 41.8, 46.0), ((2, 24576, 4096, 48), 37.4, 42.0), ((2, 24576, 8064, 48), 70.6, 84.9),
+                                                  ((2, 24576, 8320, 48), 72.3, 85.7), ((2, 20480, 24576, 48), 173.0, 188.5), ((1, 40960, 8192, 48), 61.0, 63.3),
+                                                  ((2, 17000, 8192, 48), 60.3, 57.3), ((2, 20480, 8192, 33), 64.6, 59.1), ((2, 24576, 8192, 64), 77.6, 69.8)])
+def test_tiles_of_192_rows_where_they_are_ahead(call, of_192, of_256):
+    matrices, m, n, tokens = call
+    layout = bcq.int8_layout(m, n, tokens, matrices)
+    assert (layout["rows"], layout["tokens"]) == (192 if of_192 < of_256 else 256, 64)
