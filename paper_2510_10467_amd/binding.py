@@ -369,7 +369,7 @@ def _int8_shapes(where: str, q, token_scales, mats) -> tuple:
             raise TypeError(f"{where}: codes and scales must be GPU tensors (there is no CPU path)")
         if t.device != q.device:
             raise ValueError(f"{where}: tensors on several devices")
-    if q.dim() != 2 or token_scales.shape != q.shape[:1]:
+    if q.dim() != 2 or token_scales.shape != q.shape[:1] or mats[0][0].dim() != 2:
         raise ValueError(f"{where}: inconsistent shapes")
     m, n = mats[0][0].shape[0], q.shape[1]
     for w, c in mats:
