@@ -13,7 +13,7 @@
 // Neighbouring workgroups' numbers go to different XCDs, each with a cache of its own: they are renumbered so that one XCD works on
 // the token tiles of the same weights.
 //
-// What bounds it: with every CU at work on large tiles the clock that the matrix pipe's power leaves (28672 x 8192 with 2048 tokens 445 us = 2160 TOP/s;
+// What bounds it: with every CU at work on large tiles the clock that the matrix pipe's power leaves (28672 x 8192 with 2048 tokens 445 to 465 us = 2160 to 2070 TOP/s;
 // the library's own 8-bit product of 8192^3 2100; with codes of zero a tenth less time).  With fewer tiles what LDS takes and gives: a KiB written
 // by a load takes it 16 cycles, a KiB of operands read 8.  With few tiles the latency of a step, about 0.3 us where three steps of
 // 64 x 64 are under way.  Tall matrices with 33 to 128 tokens: the CUs that the last round leaves without work, and the weights' share of
