@@ -78,7 +78,7 @@ constexpr int kTop = 14, kGatedTop = 13;                // exponents
 constexpr int kMostPower = 126;                         // of a power, either way
 constexpr float kFitsFrom = 1.f, kFitsTo = 65000.f;
 // Whether a token's first power fits, by its largest G: `some`, there is one between kFitsFrom and kFitsTo; `other`, the largest that is not, as fp32's
-// bits.  (Above kFitsTo: only where the scales' product leaves fp32.)
+// bits.  (Above kFitsTo: only where the scales' product leaves fp32 and a power is 1 at first.)
 struct TokenFit {
     uint32_t *some, *other;
 };

@@ -128,12 +128,12 @@ __global__ __launch_bounds__(256) void int8_powers_kernel(const uint16_t *__rest
     if (t >= TOKENS || token0 + t >= tokens) return;
     auto usable = [](float v) { return v > 0.f && v < __builtin_inff(); };
     const float most = fmaxf(fmaxf(tops[t][0], tops[t][1]), fmaxf(tops[t][2], tops[t][3]));
-    int e = MATS == 2 ? kGatedTop : kTop;
-    if (usable(most)) e -= ilogbf(most);
+    int e = usable(most) ? (MATS == 2 ? kGatedTop : kTop) - ilogbf(most) : 0;
     if constexpr (MATS == 2) {
         const float length = sqrtf((float)(squares[t][0] + squares[t][1] + squares[t][2] + squares[t][3]));
         const float sums = fabsf(token_scales[token0 + t]) * (1.13f * 128.f * sqrtf((float)n) * length);
-        if (usable(sums)) e -= ilogbf(sums);
+        // (with either beyond fp32 the gradients' size is anywhere: as they are at first)
+        e = usable(most) && usable(sums) ? e - ilogbf(sums) : 0;
         fit.some[token0 + t] = fit.other[token0 + t] = 0;
     }
     powers[token0 + t] = ldexpf(1.f, min(max(e, -kMostPower), kMostPower));

@@ -218,3 +218,20 @@ def test_gradients_near_either_end_of_the_type(bcq, dtype, exponents):
             close(got[0], ref, 2 * half_step(dtype) * ref.abs() + 2 * tiny(dtype), f"dx, 2^{e}")
             for a, b in zip(got[1:], want[1:]):
                 close(a, b.double() * 2.0 ** e, 2 * E32 * (b.double() * 2.0 ** e).abs() + 1e-40, f"scales, 2^{e}")
+
+
+@pytest.mark.parametrize("large, small", [(60, -60), (110, -20), (-60, 60)])
+@pytest.mark.parametrize("tokens, m, n", SIZES)
+def test_scales_whose_product_leaves_fp32(bcq, tokens, m, n, large, small):
+    """Token scales of 2^large, gradients of 2^small and channel scales that keep the projections at a few units (gate) and 2^(large - 35) (up): the
+    products of a gradient and both channel scales, or a token's bound, are beyond fp32, the gradients are not."""
+    gen = generator("product", tokens, m, n, large)
+    q, ts, [(wg, cg), (wu, cu)] = operands(tokens, m, n, gen, 2)
+    ts = ts * 2.0 ** large
+    cg = cg * 2.0 ** -large
+    cu = cu * 2.0 ** -35
+    dh = (torch.randn((tokens, m), device="cuda", generator=gen) * 2.0 ** small).bfloat16()
+    want, tol = gated64(dh, q, ts, wg, cg, wu, cu, "silu")
+    assert 2.0 ** -120 < float(want[0].abs().max()) < 2.0 ** 100
+    got = bcq.bcq_int8_gated_backward(dh, q, ts, wg, cg, wu, cu, "silu")
+    close(got[0], want[0], tol[0] + want[0].abs() * half_step(torch.bfloat16) + tiny(torch.bfloat16), "dx")
