@@ -13,7 +13,7 @@
 //
 // What bounds it: the power of the matrix pipe on random operands (2048 tokens, 4096 columns, 2 x 14336 channels: 437 to 459 us = 1100 to 1050 TFLOP/s,
 // with gradients of zero 330; the library's plain binary16 product of 8192^3 1300), the codes' conversion beside it, and with few tokens
-// the weights' bytes (17920 x 5120, gated, 48 tokens: 47 us = 3.9 TB/s).  The whole gated backward pass of 2048 tokens: 729 to 741 us; the
+// the weights' bytes (17920 x 5120, gated, 48 tokens: 47 us = 3.9 TB/s).  The whole gated backward pass of 2048 tokens: 713 to 745 us; the
 // profiler, which counts the time that two launches overlap twice, has 18 for the powers, 295 for the first half, 5 for the second look with the sums, 447
 // for the second half.
 #include <math.h>
